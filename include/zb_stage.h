@@ -318,6 +318,121 @@ zb_status zb_optimizer_step_validated(zb_stage* st, const zb_global_state* gs, z
 zb_status zb_grad_norm_static(const float* grads, size_t n, double* sq_out, int32_t* nonfinite_out,
                               void* hip_stream);
 
+/* ---- Operators of a post-training step, on device memory of the caller ------------------------------
+ * Log-probabilities of given tokens, two losses on them with the gradient of the logits, AdamW over many
+ * tensors.  No stage is needed; the calls only enqueue kernels (no synchronisation, allocation or memset), so
+ * they may be captured into a graph.  They run on `hip_stream` (NULL: the default stream of the current device)
+ * and on the device that stream belongs to, whichever is current.  ZB_EINVAL: an argument is outside what is
+ * said here, nothing is launched then; ZB_EDEVICE: a HIP call failed.
+ *
+ * The logits of `rows` tokens: row r starts at element r * row_stride, row_stride >= vocab, any alignment of the
+ * data type; targets[r] is the token whose log-probability counts.  A row whose target lies outside [0, vocab)
+ * (padding: -1) does not count: its logits are not read, its log-probability is given as 0 and its gradient row as
+ * zeros.  A logit of -infinity has probability 0; a row of nothing else, or with a NaN or +infinity, gives NaN.
+ * rows may be 0. */
+typedef struct {
+  const void* logits;      /* device */
+  const int32_t* targets;  /* device, [rows] */
+  int64_t row_stride;      /* elements, <= 2^32 */
+  int32_t rows, vocab;     /* rows <= 2^24, 1 <= vocab <= 2^18 */
+  int32_t dtype;           /* zb_dtype of logits and gradient */
+} zb_logits;
+
+/* logp[r] = logit of the target - lse[r], lse[r] = log of the sum of the row's exponentials; lse may be NULL. */
+zb_status zb_token_logprobs(const zb_logits* x, float* logp, float* lse, void* hip_stream);
+
+/* dlogits[r, j] = dlogp[r] * ([j == targets[r]] - exp(logits[r, j] - lse[r])), with zb_token_logprobs' lse.  A row
+ * whose dlogp is 0 is not read and gets zeros.  dlogits may be the logits themselves (then with the same stride);
+ * dlogits_stride 0 stands for x->row_stride.  Only [rows, vocab] is written. */
+zb_status zb_token_logprobs_backward(const zb_logits* x, const float* lse, const float* dlogp, void* dlogits,
+                                     int64_t dlogits_stride, void* hip_stream);
+
+/* Scratch that the two losses need (device, 8-byte aligned, zero before its first use).
+ * Calls that may run at the same time, replays of captured ones among them, need one each. */
+zb_status zb_loss_workspace_bytes(int32_t rows, int32_t pairs, size_t* bytes);
+
+/* Clipped policy loss with a KL term: with rho = exp(logp - old_logp) and d = ref_logp - logp,
+ *   loss = scale * sum over the rows of weight * (-min(rho A, clip(rho, 1 - clip_low, 1 + clip_high) A)
+ *                                                 + kl_coef * (exp(d) - d - 1)),   A = advantage,
+ * and its gradient with respect to the logits (old_logp, ref_logp and A are constants).  Where the clipped term is
+ * the smaller one it passes no gradient.  A row of weight 0 does not count (as above: nothing of it is read, its old_logp,
+ * ref_logp and advantage included). */
+typedef struct {
+  const float *old_logp, *advantage; /* device, [rows] */
+  const float* ref_logp;             /* device, [rows]; may be NULL if kl_coef is 0 */
+  const float* weight;               /* device, [rows], or NULL: 1 each */
+  double clip_low, clip_high;        /* 0 <= clip_low <= 1, clip_high >= 0 */
+  double kl_coef, scale;             /* kl_coef >= 0 */
+} zb_policy;
+/* loss: device, one fp32.  logp ([rows]) and dlogits may be NULL; dlogits may be the logits, as above. */
+zb_status zb_policy_loss(const zb_logits* x, const zb_policy* p, float* loss, float* logp, void* dlogits,
+                         int64_t dlogits_stride, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Preference loss of pairs of sequences, the preferred one first: sequence q holds rows offsets[q] .. offsets[q + 1] - 1 (none
+ * is allowed), S_q = the sum over its rows of weight * (logp - ref_logp), x = beta * (S_2i - S_2i+1),
+ *   loss = scale * sum over i of -(1 - label_smoothing) log sigma(x) - label_smoothing log sigma(-x).
+ * Rows of weight 0 and rows before the first or behind the last sequence do not count. */
+typedef struct {
+  const float* ref_logp;   /* device, [rows] */
+  const float* weight;     /* device, [rows], or NULL: 1 each */
+  const int32_t* offsets;  /* device, [2 * pairs + 1], not decreasing, in [0, rows] */
+  int32_t pairs;           /* may be 0 */
+  double beta, label_smoothing, scale; /* 0 <= label_smoothing <= 1 */
+} zb_preference;
+/* rewards: device, [2 * pairs], beta * S_q, or NULL; the others as for zb_policy_loss. */
+zb_status zb_preference_loss(const zb_logits* x, const zb_preference* p, float* loss, float* logp, float* rewards,
+                             void* dlogits, int64_t dlogits_stride, void* workspace, size_t workspace_bytes,
+                             void* hip_stream);
+
+/* AdamW over many tensors at once (zb_optimizer_step_validated's step without its protocol), each anywhere in device
+ * memory.  With 32-bit states m and v are float[n].  With 8-bit states m is int8[n], v is uint8[n], and every 256
+ * consecutive values of a tensor (the last block may be shorter) share one float in m_scale and one in v_scale,
+ * the block's largest |m| and v:  m = sign(c) (c / 127)^2 m_scale,  v = (c / 255)^4 v_scale.  Values are rounded up or
+ * down at random so that the mean is kept, by numbers made of seed, the step and the value's place first + index
+ * alone: a step gives the same bits on every run, and tensors of one program should not share places.  All-zero
+ * states are the states before the first step.  A tensor may be listed once only. */
+typedef struct {
+  float* theta;       /* parameters, fp32 */
+  const void* grad;   /* their gradients */
+  void* copy16;       /* bf16 working copy of theta that the step refreshes, or NULL */
+  void *m, *v;        /* moments */
+  float *m_scale, *v_scale; /* 8-bit states: [(n + 255) / 256] each; otherwise unused */
+  int64_t n;          /* values; 0 is allowed */
+  int64_t first;      /* place of value 0 in the random sequence, >= 0 */
+  int32_t grad_dtype; /* zb_dtype */
+  int32_t decay;      /* 0: no weight decay for this tensor */
+} zb_adamw_tensor;
+typedef struct {
+  int32_t bits;       /* 8 or 32 */
+  uint32_t seed;
+  double beta1, beta2, eps, weight_decay;
+  double clip;        /* threshold of the gradient norm, > 0; infinity: none */
+} zb_adamw_config;
+
+/* Squared norm and non-finite flag of all gradients listed (theta, m, v are not looked at), as zb_grad_norm_static gives
+ * them: sq_out one double, nonfinite_out one int32, both on the device; sums in a fixed order.  The workspace is device
+ * memory, 8-byte aligned, zero before its first use, of its own for calls that may run at the same time. */
+zb_status zb_adamw_workspace_bytes(const zb_adamw_tensor* tensors, int32_t count, size_t* bytes);
+zb_status zb_adamw_grad_norm(const zb_adamw_tensor* tensors, int32_t count, double* sq_out, int32_t* nonfinite_out,
+                             void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* One step.  state: ZB_ADAMW_STATE_BYTES of device memory, 8-byte aligned, zero before the first step; its first 8 bytes
+ * hold the number of steps taken as an int64 (a caller that resumes writes it there).  sq and nonfinite (device, both or
+ * neither): the squared norm and the flag of all gradients that are clipped together, of this list or of more; the
+ * gradients are scaled by min(1, clip / (sqrt(sq) + 1e-6)), and if the flag is set or sq is not finite nothing changes,
+ * the number of steps included.  8-bit states need them: they cannot hold a NaN. */
+#define ZB_ADAMW_STATE_BYTES 64
+zb_status zb_adamw_step(const zb_adamw_config* cfg, const zb_adamw_tensor* tensors, int32_t count, double lr, void* state,
+                        const double* sq, const int32_t* nonfinite, void* hip_stream);
+
+/* Moments held in 8 bits as fp32 values and back (each to the nearer code), e.g. for a checkpoint: values[k].m and .v
+ * are device arrays of tensors[k].n floats; theta and grad are not looked at. */
+typedef struct {
+  float *m, *v;
+} zb_adamw_value;
+zb_status zb_adamw_read_moments(const zb_adamw_tensor* tensors, int32_t count, const zb_adamw_value* values, void* hip_stream);
+zb_status zb_adamw_write_moments(const zb_adamw_tensor* tensors, int32_t count, const zb_adamw_value* values, void* hip_stream);
+
 /* Copies between host fp32 buffers and stage tensors (converting to/from the stage's
  * data type).  bytes must equal 4 * number of elements.  Both wait for the device. */
 zb_status zb_get_tensor(zb_stage* st, int32_t what, int32_t layer, int32_t mb, void* host_dst, size_t bytes);

@@ -83,6 +83,36 @@ class zb_kernel_stat(C.Structure):
                 ("flops", C.c_double), ("bytes", C.c_double)]
 
 
+class zb_logits(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("targets", C.c_void_p), ("row_stride", C.c_int64), ("rows", C.c_int32),
+                ("vocab", C.c_int32), ("dtype", C.c_int32)]
+
+
+class zb_policy(C.Structure):
+    _fields_ = [("old_logp", C.c_void_p), ("advantage", C.c_void_p), ("ref_logp", C.c_void_p), ("weight", C.c_void_p),
+                ("clip_low", C.c_double), ("clip_high", C.c_double), ("kl_coef", C.c_double), ("scale", C.c_double)]
+
+
+class zb_preference(C.Structure):
+    _fields_ = [("ref_logp", C.c_void_p), ("weight", C.c_void_p), ("offsets", C.c_void_p), ("pairs", C.c_int32),
+                ("beta", C.c_double), ("label_smoothing", C.c_double), ("scale", C.c_double)]
+
+
+class zb_adamw_tensor(C.Structure):
+    _fields_ = [("theta", C.c_void_p), ("grad", C.c_void_p), ("copy16", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("n", C.c_int64), ("first", C.c_int64),
+                ("grad_dtype", C.c_int32), ("decay", C.c_int32)]
+
+
+class zb_adamw_config(C.Structure):
+    _fields_ = [("bits", C.c_int32), ("seed", C.c_uint32), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("weight_decay", C.c_double), ("clip", C.c_double)]
+
+
+class zb_adamw_value(C.Structure):
+    _fields_ = [("m", C.c_void_p), ("v", C.c_void_p)]
+
+
 _P = C.POINTER
 _sig = {
     "zb_config_defaults": [_P(zb_config)],
@@ -126,6 +156,19 @@ _sig = {
     "zb_profile_enable": [C.c_void_p, C.c_int32],
     "zb_profile_read": [C.c_void_p, _P(zb_kernel_stat), C.c_int32, _P(C.c_int32)],
     "zb_grad_norm_static": [C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p, C.c_void_p],
+    "zb_token_logprobs": [_P(zb_logits), C.c_void_p, C.c_void_p, C.c_void_p],
+    "zb_token_logprobs_backward": [_P(zb_logits), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p],
+    "zb_loss_workspace_bytes": [C.c_int32, C.c_int32, _P(C.c_size_t)],
+    "zb_policy_loss": [_P(zb_logits), _P(zb_policy), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t,
+                       C.c_void_p],
+    "zb_preference_loss": [_P(zb_logits), _P(zb_preference), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64,
+                           C.c_void_p, C.c_size_t, C.c_void_p],
+    "zb_adamw_workspace_bytes": [_P(zb_adamw_tensor), C.c_int32, _P(C.c_size_t)],
+    "zb_adamw_grad_norm": [_P(zb_adamw_tensor), C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p],
+    "zb_adamw_step": [_P(zb_adamw_config), _P(zb_adamw_tensor), C.c_int32, C.c_double, C.c_void_p, C.c_void_p, C.c_void_p,
+                      C.c_void_p],
+    "zb_adamw_read_moments": [_P(zb_adamw_tensor), C.c_int32, _P(zb_adamw_value), C.c_void_p],
+    "zb_adamw_write_moments": [_P(zb_adamw_tensor), C.c_int32, _P(zb_adamw_value), C.c_void_p],
 }
 for _name, _args in _sig.items():
     _f = getattr(lib, _name)
@@ -292,6 +335,137 @@ def grad_norm_static(grads_ptr: int, n: int, sq_out_ptr: int, nonfinite_out_ptr:
     rc = lib.zb_grad_norm_static(grads_ptr, n, sq_out_ptr, nonfinite_out_ptr, stream_handle or None)
     if rc != OK:
         raise ZbError(rc, "zb_grad_norm_static")
+
+
+# ---- operators of a post-training step: all pointers are device addresses (ints, 0: none), stream_handle a hipStream_t or 0 ----
+DTYPE = {"fp32": FP32, "bf16": BF16}
+ADAMW_STATE_BYTES = 64
+
+
+def logits(logits_ptr: int, rows: int, vocab: int, targets_ptr: int, dtype: str = "bf16", row_stride: int = 0) -> zb_logits:
+    """zb_logits; row_stride 0: the rows are dense."""
+    return zb_logits(logits_ptr, targets_ptr, row_stride or vocab, rows, vocab, DTYPE[dtype])
+
+
+def policy(old_logp: int, advantage: int, ref_logp: int = 0, weight: int = 0, clip_low: float = 0.2, clip_high: float = 0.2,
+           kl_coef: float = 0.0, scale: float = 1.0) -> zb_policy:
+    """zb_policy."""
+    return zb_policy(old_logp, advantage, ref_logp, weight, clip_low, clip_high, kl_coef, scale)
+
+
+def preference(ref_logp: int, offsets: int, pairs: int, weight: int = 0, beta: float = 0.1, label_smoothing: float = 0.0,
+               scale: float = 1.0) -> zb_preference:
+    """zb_preference."""
+    return zb_preference(ref_logp, weight, offsets, pairs, beta, label_smoothing, scale)
+
+
+def token_logprobs(x: zb_logits, logp_ptr: int, lse_ptr: int = 0, stream_handle: int = 0):
+    """zb_token_logprobs."""
+    rc = lib.zb_token_logprobs(x, logp_ptr, lse_ptr, stream_handle)
+    if rc != OK:
+        raise ZbError(rc, "zb_token_logprobs")
+
+
+def token_logprobs_backward(x: zb_logits, lse_ptr: int, dlogp_ptr: int, dlogits_ptr: int, dlogits_stride: int = 0,
+                            stream_handle: int = 0):
+    """zb_token_logprobs_backward."""
+    rc = lib.zb_token_logprobs_backward(x, lse_ptr, dlogp_ptr, dlogits_ptr, dlogits_stride, stream_handle)
+    if rc != OK:
+        raise ZbError(rc, "zb_token_logprobs_backward")
+
+
+def loss_workspace_bytes(rows: int, pairs: int = 0) -> int:
+    """zb_loss_workspace_bytes."""
+    n = C.c_size_t(0)
+    rc = lib.zb_loss_workspace_bytes(rows, pairs, C.byref(n))
+    if rc != OK:
+        raise ZbError(rc, "zb_loss_workspace_bytes")
+    return n.value
+
+
+def policy_loss(x: zb_logits, p: zb_policy, loss_ptr: int, logp_ptr: int = 0, dlogits_ptr: int = 0, dlogits_stride: int = 0, *,
+                workspace: int, workspace_bytes: int, stream_handle: int = 0):
+    """zb_policy_loss."""
+    rc = lib.zb_policy_loss(x, p, loss_ptr, logp_ptr, dlogits_ptr, dlogits_stride, workspace, workspace_bytes, stream_handle)
+    if rc != OK:
+        raise ZbError(rc, "zb_policy_loss")
+
+
+def preference_loss(x: zb_logits, p: zb_preference, loss_ptr: int, logp_ptr: int = 0, rewards_ptr: int = 0, dlogits_ptr: int = 0,
+                    dlogits_stride: int = 0, *, workspace: int, workspace_bytes: int, stream_handle: int = 0):
+    """zb_preference_loss."""
+    rc = lib.zb_preference_loss(x, p, loss_ptr, logp_ptr, rewards_ptr, dlogits_ptr, dlogits_stride, workspace, workspace_bytes,
+                                stream_handle)
+    if rc != OK:
+        raise ZbError(rc, "zb_preference_loss")
+
+
+def adamw_config(bits: int = 32, beta1: float = 0.9, beta2: float = 0.95, eps: float = 1e-8, weight_decay: float = 0.01,
+                 clip: float = 1.0, seed: int = 0) -> zb_adamw_config:
+    """zb_adamw_config, the stage's hyperparameters by default."""
+    return zb_adamw_config(bits, seed, beta1, beta2, eps, weight_decay, clip)
+
+
+def adamw_tensors(tensors) -> "C.Array":
+    """Array of zb_adamw_tensor from dicts of its fields (grad_dtype "fp32" or "bf16", decay on by default)."""
+    out = (zb_adamw_tensor * len(tensors))()
+    for q, t in zip(out, tensors):
+        t = dict(t)
+        q.grad_dtype = DTYPE[t.pop("grad_dtype", "fp32")]
+        q.decay = int(t.pop("decay", True))
+        for name in ("theta", "grad", "m", "v", "m_scale", "v_scale", "copy16", "n", "first"):
+            if name in t:
+                setattr(q, name, t.pop(name))
+        if t:
+            raise TypeError(f"unknown field {sorted(t)[0]!r} of an adamw tensor")
+    return out
+
+
+def adamw_values(values) -> "C.Array":
+    """Array of zb_adamw_value from (address of m's values, address of v's values) pairs."""
+    return (zb_adamw_value * len(values))(*values)
+
+
+def adamw_workspace_bytes(tensors) -> int:
+    """zb_adamw_workspace_bytes."""
+    n = C.c_size_t(0)
+    rc = lib.zb_adamw_workspace_bytes(tensors, len(tensors), C.byref(n))
+    if rc != OK:
+        raise ZbError(rc, "zb_adamw_workspace_bytes")
+    return n.value
+
+
+def adamw_grad_norm(tensors, sq_ptr: int, nonfinite_ptr: int, *, workspace: int, workspace_bytes: int, stream_handle: int = 0):
+    """zb_adamw_grad_norm."""
+    rc = lib.zb_adamw_grad_norm(tensors, len(tensors), sq_ptr, nonfinite_ptr, workspace, workspace_bytes, stream_handle)
+    if rc != OK:
+        raise ZbError(rc, "zb_adamw_grad_norm")
+
+
+def adamw_step(config: zb_adamw_config, tensors, lr: float, state_ptr: int, sq_ptr: int = 0, nonfinite_ptr: int = 0,
+               stream_handle: int = 0):
+    """zb_adamw_step."""
+    rc = lib.zb_adamw_step(config, tensors, len(tensors), lr, state_ptr, sq_ptr, nonfinite_ptr, stream_handle)
+    if rc != OK:
+        raise ZbError(rc, "zb_adamw_step")
+
+
+def adamw_read_moments(tensors, values, stream_handle: int = 0):
+    """zb_adamw_read_moments."""
+    if len(values) != len(tensors):
+        raise ZbError(EINVAL, "adamw_read_moments: one pair of values for each tensor")
+    rc = lib.zb_adamw_read_moments(tensors, len(tensors), values, stream_handle)
+    if rc != OK:
+        raise ZbError(rc, "zb_adamw_read_moments")
+
+
+def adamw_write_moments(tensors, values, stream_handle: int = 0):
+    """zb_adamw_write_moments."""
+    if len(values) != len(tensors):
+        raise ZbError(EINVAL, "adamw_write_moments: one pair of values for each tensor")
+    rc = lib.zb_adamw_write_moments(tensors, len(tensors), values, stream_handle)
+    if rc != OK:
+        raise ZbError(rc, "zb_adamw_write_moments")
 
 
 @dataclass

@@ -78,6 +78,23 @@ template <> __device__ __forceinline__ float gelu_grad<bf16_t>(float x) {
   return x < 0.0f ? -(w * k) : fmaf(w, k, 1.0f);
 }
 
+// the device that a stream belongs to is current while this lives
+struct OnDeviceOf {
+  int before = -1;
+  bool ok = true;
+  explicit OnDeviceOf(hipStream_t s) {
+    if (!s) return;
+    int now = -1;
+    hipDevice_t dev = -1;
+    if (hipGetDevice(&now) != hipSuccess || hipStreamGetDevice(s, &dev) != hipSuccess) { ok = false; return; }
+    if ((int)dev != now) {
+      ok = hipSetDevice((int)dev) == hipSuccess;
+      if (ok) before = now;
+    }
+  }
+  ~OnDeviceOf() { if (before >= 0) (void)hipSetDevice(before); }
+};
+
 // ---------------------------------------------------------------------------------------
 // GEMM:  C[M,N] (op)= sum_k A(m,k) * B(k,n).   A element (m,k) sits at A[m*a_sm + k*a_sk],
 // B element (k,n) at B[k*b_sk + n*b_sn]; exactly one stride of each operand is 1.
