@@ -13,6 +13,7 @@ namespace zb {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr float kLog2e = 1.44269504f;
 
 struct Rows {
   const int* targets;
@@ -26,63 +27,92 @@ struct Rows {
   __device__ __forceinline__ double weight_of(int row) const { return weight ? (double)weight[row] : 1.0; }
 };
 
-// (m, s) stands for s * exp(m); an empty or all -infinity part has m = -infinity and s = 0
-__device__ __forceinline__ void lse_merge(float& m, float& s, float m2, float s2) {
-  const float top = fmaxf(m, m2);
-  s = (m == -INFINITY ? 0.f : s * __expf(m - top)) + (m2 == -INFINITY ? 0.f : s2 * __expf(m2 - top));
-  m = top;
+// A row as it lies in memory: `head` elements up to the first address that is a multiple of 16, `full` 16-byte vectors, `tail`
+// elements.  The elements before and behind the vectors are at most VE - 1 each and belong to the first 2 VE lanes.
+template <typename T> struct Span {
+  static constexpr int VE = 16 / sizeof(T);
+  int head, full, tail;
+  __device__ __forceinline__ Span(const T* row, int vocab) {
+    head = (int)(((16 - ((uintptr_t)row & 15)) & 15) / sizeof(T));
+    if (head > vocab) head = vocab;
+    full = (vocab - head) / VE;
+    tail = vocab - head - full * VE;
+  }
+  // index of the element that this lane has beside the vectors, -1 for none
+  __device__ __forceinline__ int edge(int lane) const {
+    if (lane < VE) return lane < head ? lane : -1;
+    return lane - VE < tail ? head + full * VE + lane - VE : -1;  // (tail < VE: lanes from 2 VE on have none)
+  }
+};
+template <typename T> __device__ __forceinline__ void unpack(const uint4& r, float (&x)[16 / sizeof(T)]);
+template <> __device__ __forceinline__ void unpack<float>(const uint4& r, float (&x)[4]) {
+  x[0] = __uint_as_float(r.x); x[1] = __uint_as_float(r.y); x[2] = __uint_as_float(r.z); x[3] = __uint_as_float(r.w);
+}
+template <> __device__ __forceinline__ void unpack<bf16_t>(const uint4& r, float (&x)[8]) {
+  const unsigned w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+}
+template <typename T> __device__ __forceinline__ uint4 pack(const float (&x)[16 / sizeof(T)]);
+template <> __device__ __forceinline__ uint4 pack<float>(const float (&x)[4]) {
+  return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+}
+template <> __device__ __forceinline__ uint4 pack<bf16_t>(const float (&x)[8]) {
+  union { bf16x8 v; uint4 u; } c;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) c.v[i] = (bf16_t)x[i];
+  return c.u;
+}
+template <typename T> __device__ __forceinline__ uint4 empty_pack();  // all -infinity
+template <> __device__ __forceinline__ uint4 empty_pack<float>() { return make_uint4(0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u); }
+template <> __device__ __forceinline__ uint4 empty_pack<bf16_t>() { return make_uint4(0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u); }
+
+// Keeps a row as it was loaded: without it the 32-bit forms of one pass over it are kept for the next, in twice the registers.
+template <int NV> __device__ __forceinline__ void as_loaded(uint4 (&r)[NV]) {
+#pragma unroll
+  for (int i = 0; i < NV; ++i) asm volatile("" : "+v"(r[i].x), "+v"(r[i].y), "+v"(r[i].z), "+v"(r[i].w));
 }
 
-// lse and log-probability of a row, by one workgroup
-template <typename T>
-__global__ __launch_bounds__(kThreads) void row_logp_kernel(const T* __restrict__ logits, long stride, Rows of, float* __restrict__ logp,
-                                                            float* __restrict__ lse) {
-  __shared__ float red_m[kThreads / 64], red_s[kThreads / 64];
-  const int row = blockIdx.x;
-  const int vocab = of.vocab;
-  if (!of.counts(row)) {
-    if (threadIdx.x == 0) { if (logp) logp[row] = 0.f; if (lse) lse[row] = 0.f; }
-    return;
-  }
-  const T* z = logits + (long)row * stride;
-  float m = -INFINITY, s = 0.f;
-  for (int c = threadIdx.x; c < vocab; c += kThreads) {
-    const float x = to_f32(z[c]);
-    if (x != x) { m = x; s = x; }  // a NaN stays
-    else if (m == m) lse_merge(m, s, x, 1.f);
-  }
-  for (int o = 32; o > 0; o >>= 1) {
-    const float m2 = __shfl_xor(m, o, 64), s2 = __shfl_xor(s, o, 64);
-    if (m2 != m2 || m != m) { m = NAN; s = NAN; }
-    else lse_merge(m, s, m2, s2);
-  }
-  if ((threadIdx.x & 63) == 0) { red_m[threadIdx.x >> 6] = m; red_s[threadIdx.x >> 6] = s; }
+__device__ __forceinline__ float exp_of(float x, float top) { return __builtin_amdgcn_exp2f((x - top) * kLog2e); }
+// log(s) of 1 <= s < 2^19 (or NaN), off by 3e-8: the exponent apart, so that no digits go to it
+__device__ __forceinline__ double log_of(float s) {
+  const int e = (int)(__float_as_uint(s) >> 23) - 127;
+  const float f = __uint_as_float((__float_as_uint(s) & 0x007FFFFFu) | 0x3F800000u);
+  const bool up = f > 1.41421356f;
+  const double l = (double)(e + (up ? 1 : 0)) + (double)__builtin_amdgcn_logf(up ? 0.5f * f : f);
+  return s == s ? l * 0.6931471805599453 : (double)s;
+}
+
+// what the lanes of a workgroup of N waves hold, reduced in a fixed order; `red` is read after the barrier only
+template <int N> __device__ __forceinline__ float block_max(float v, float* red) {
+  v = wave_max(v);
+  if (N == 1) return v;
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
-  if (threadIdx.x) return;
-  m = red_m[0]; s = red_s[0];
-  for (int w = 1; w < kThreads / 64; ++w) {
-    if (red_m[w] != red_m[w] || m != m) { m = NAN; s = NAN; }
-    else lse_merge(m, s, red_m[w], red_s[w]);
-  }
-  if (m == -INFINITY) s = NAN;  // a row of nothing but -infinity has no softmax
-  const double ls = log((double)s);
-  if (lse) lse[row] = (float)((double)m + ls);
-  if (logp) logp[row] = (float)(((double)to_f32(z[of.targets[row]]) - (double)m) - ls);
+  v = red[0];
+#pragma unroll
+  for (int w = 1; w < N; ++w) v = fmaxf(v, red[w]);
+  return v;
+}
+template <int N> __device__ __forceinline__ float block_sum(float v, float* red) {
+  v = wave_sum(v);
+  if (N == 1) return v;
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = red[0];
+#pragma unroll
+  for (int w = 1; w < N; ++w) v += red[w];
+  return v;
 }
 
-// coef ([j = target] - exp(z_j - lse)), or zeros where the row does not count
-template <typename T>
-__global__ __launch_bounds__(kThreads) void row_grad_kernel(const T* logits, long stride, Rows of, const float* __restrict__ lse,
-                                                            const float* __restrict__ coef, T* dlogits, long dstride) {
-  const int row = blockIdx.x;
-  const int vocab = of.vocab, t = of.targets[row];
-  const float k = of.counts(row) ? coef[row] : 0.f;
-  const bool counts = k != 0.f;  // (also NaN)
-  const float l = counts ? lse[row] : 0.f;
-  const T* z = logits + (long)row * stride;
-  T* d = dlogits + (long)row * dstride;
-  for (int c = threadIdx.x; c < vocab; c += kThreads)
-    d[c] = counts ? from_f32<T>(k * ((c == t ? 1.f : 0.f) - __expf(to_f32(z[c]) - l))) : from_f32<T>(0.f);
+// zeros in a row's gradient, by THREADS lanes
+template <typename T> __device__ __forceinline__ void clear_row(T* d, int vocab, int threads) {
+  const Span<T> sp(d, vocab);
+  const int lane = threadIdx.x;
+  uint4* v = reinterpret_cast<uint4*>(d + sp.head);
+  for (int k = lane; k < sp.full; k += threads) v[k] = make_uint4(0, 0, 0, 0);
+  const int e = sp.edge(lane);
+  if (e >= 0) d[e] = from_f32<T>(0.f);
 }
 
 struct PolicyArgs {
@@ -105,15 +135,265 @@ __device__ __forceinline__ double policy_row(const PolicyArgs& a, const Rows& of
   return w * loss;
 }
 
-__global__ __launch_bounds__(kThreads) void policy_coef_kernel(PolicyArgs a, Rows of, int rows,
-                                                               const float* __restrict__ logp, float* __restrict__ coef,
-                                                               double* __restrict__ part) {
-  const int row = blockIdx.x * kThreads + threadIdx.x;
-  if (row >= rows) return;
-  double slope = 0.0, loss = 0.0;
-  if (of.counts(row)) loss = policy_row(a, of, row, logp[row], &slope);
-  coef[row] = (float)slope;
-  part[row] = loss;
+struct RowOut {  // what the row kernels leave of a row; null: not wanted
+  float *logp, *lse;
+  float *top, *inv;  // p_j = exp(z_j - top) * inv
+  double *logp64;    // logp before its rounding
+  double *part;      // with a policy: its loss
+};
+__device__ __forceinline__ void put_row(const RowOut& o, int row, double logp, double lse, float top, float s) {
+  if (o.logp) o.logp[row] = (float)logp;
+  if (o.lse) o.lse[row] = (float)lse;
+  if (o.top) { o.top[row] = top; o.inv[row] = 1.0f / s; }
+  if (o.logp64) o.logp64[row] = logp;
+}
+__device__ __forceinline__ void put_no_row(const RowOut& o, int row) {
+  if (o.logp) o.logp[row] = 0.f;
+  if (o.lse) o.lse[row] = 0.f;
+  if (o.top) { o.top[row] = 0.f; o.inv[row] = 0.f; }
+  if (o.logp64) o.logp64[row] = 0.0;
+  if (o.part) o.part[row] = 0.0;
+}
+
+// One workgroup per row, the row in registers (NV vectors a lane): read once for the maximum, the sum and, with POLICY, the
+// gradient that follows from the row's own log-probability.
+template <typename T, int THREADS, int NV, bool POLICY>
+__global__ __launch_bounds__(THREADS) void row_kernel(const T* logits, long stride, Rows of, RowOut out, PolicyArgs pol, T* dlogits, long dstride) {
+  constexpr int VE = Span<T>::VE, N = THREADS / 64;
+  __shared__ float red_m[N], red_s[N], coef_of;
+  const int row = blockIdx.x, lane = threadIdx.x;
+  T* d = dlogits + (long)row * dstride;
+  if (!of.counts(row)) {
+    if (lane == 0) put_no_row(out, row);
+    if (POLICY && dlogits) clear_row<T>(d, of.vocab, THREADS);
+    return;
+  }
+  const T* z = logits + (long)row * stride;
+  const Span<T> sp(z, of.vocab);
+  const uint4* v = reinterpret_cast<const uint4*>(z + sp.head);
+  uint4 r[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int k = i * THREADS + lane;
+    r[i] = k < sp.full ? v[k] : empty_pack<T>();
+  }
+  const int edge = sp.edge(lane);
+  const float xe = edge >= 0 ? to_f32(z[edge]) : -INFINITY;
+  const int target = of.targets[row];
+  const float zy = to_f32(z[target]);
+  float m = xe;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    float x[VE];
+    unpack<T>(r[i], x);
+#pragma unroll
+    for (int e = 0; e < VE; ++e) m = fmaxf(m, x[e]);
+  }
+  m = block_max<N>(m, red_m);
+  as_loaded(r);
+  float s0 = exp_of(xe, m), s1 = 0.f;  // (a NaN, an infinity and a row of nothing but -infinity make the sum NaN)
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    float x[VE];
+    unpack<T>(r[i], x);
+#pragma unroll
+    for (int e = 0; e < VE; e += 2) { s0 += exp_of(x[e], m); s1 += exp_of(x[e + 1], m); }
+  }
+  const float s = block_sum<N>(s0 + s1, red_s);
+  if (!POLICY) {
+    if (lane == 0) {
+      const double l = log_of(s);
+      put_row(out, row, ((double)zy - (double)m) - l, (double)m + l, m, s);
+    }
+    return;
+  }
+  if (lane == 0) {
+    const double l = log_of(s), lp = ((double)zy - (double)m) - l;
+    double slope;
+    out.part[row] = policy_row(pol, of, row, lp, &slope);
+    put_row(out, row, lp, (double)m + l, m, s);
+    coef_of = (float)slope;
+  }
+  if (!dlogits) return;
+  __syncthreads();
+  const float coef = coef_of, neg = -coef / s;
+  if (coef == 0.f) {
+    clear_row<T>(d, of.vocab, THREADS);
+    return;
+  }
+  const bool same = (((uintptr_t)d ^ (uintptr_t)z) & 15) == 0;
+  as_loaded(r);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int k = i * THREADS + lane;
+    if (k >= sp.full) break;
+    float x[VE];
+    unpack<T>(r[i], x);
+#pragma unroll
+    for (int e = 0; e < VE; ++e) x[e] = neg * exp_of(x[e], m);
+    T* at = d + sp.head + k * VE;
+    if (same) {
+      *reinterpret_cast<uint4*>(at) = pack<T>(x);
+    } else {
+#pragma unroll
+      for (int e = 0; e < VE; ++e) at[e] = from_f32<T>(x[e]);
+    }
+  }
+  if (edge >= 0) d[edge] = from_f32<T>(neg * exp_of(xe, m));
+  // the lane that wrote the target's entry writes it again, whole
+  const int kt = target - sp.head;
+  if (kt >= 0 && kt < sp.full * VE ? (kt / VE) % THREADS == lane : edge == target) d[target] = from_f32<T>(coef * (1.f - exp_of(zy, m) / s));
+}
+
+// The same for rows that registers do not hold: read once for maximum and sum together, and again for the gradient.
+template <typename T, bool POLICY>
+__global__ __launch_bounds__(1024) void long_row_kernel(const T* logits, long stride, Rows of, RowOut out, PolicyArgs pol, T* dlogits, long dstride) {
+  constexpr int VE = Span<T>::VE, THREADS = 1024, N = THREADS / 64, U = 4;
+  __shared__ float red_m[N], red_s[N], coef_of;
+  const int row = blockIdx.x, lane = threadIdx.x;
+  T* d = dlogits + (long)row * dstride;
+  if (!of.counts(row)) {
+    if (lane == 0) put_no_row(out, row);
+    if (POLICY && dlogits) clear_row<T>(d, of.vocab, THREADS);
+    return;
+  }
+  const T* z = logits + (long)row * stride;
+  const Span<T> sp(z, of.vocab);
+  const uint4* v = reinterpret_cast<const uint4*>(z + sp.head);
+  const int edge = sp.edge(lane), target = of.targets[row];
+  const float xe = edge >= 0 ? to_f32(z[edge]) : -INFINITY, zy = to_f32(z[target]);
+  float mine = xe, part = edge >= 0 ? 1.f : 0.f;  // the lane's sum counts exp(x - mine)
+  if (xe != xe) part = xe;
+  for (int k0 = lane; k0 < sp.full; k0 += U * THREADS) {
+    uint4 r[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) r[i] = k0 + i * THREADS < sp.full ? v[k0 + i * THREADS] : empty_pack<T>();
+    float top = mine;
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      float x[VE];
+      unpack<T>(r[i], x);
+#pragma unroll
+      for (int e = 0; e < VE; ++e) top = fmaxf(top, x[e]);
+    }
+    if (top > mine) {
+      part = mine == -INFINITY ? (part != part ? part : 0.f) : part * exp_of(mine, top);
+      mine = top;
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      float x[VE];
+      unpack<T>(r[i], x);
+#pragma unroll
+      for (int e = 0; e < VE; ++e) part += mine == -INFINITY ? (x[e] != x[e] ? x[e] : 0.f) : exp_of(x[e], mine);
+    }
+  }
+  const float m = block_max<N>(mine, red_m);
+  // lanes without a finite logit add nothing, unless they saw a NaN; a row without one is undefined
+  const float own = mine == -INFINITY && m > -INFINITY ? (part != part ? part : 0.f) : part * exp_of(mine, m);
+  const float s = block_sum<N>(own, red_s);
+  if (lane == 0) {
+    const double l = log_of(s), lp = ((double)zy - (double)m) - l;
+    if (POLICY) {
+      double slope;
+      out.part[row] = policy_row(pol, of, row, lp, &slope);
+      coef_of = (float)slope;
+    }
+    put_row(out, row, lp, (double)m + l, m, s);
+  }
+  if (!POLICY || !dlogits) return;
+  __syncthreads();
+  const float coef = coef_of, neg = -coef / s;
+  if (coef == 0.f) {
+    clear_row<T>(d, of.vocab, THREADS);
+    return;
+  }
+  const bool same = (((uintptr_t)d ^ (uintptr_t)z) & 15) == 0;
+  for (int k = lane; k < sp.full; k += THREADS) {  // (a lane reads its entries before it writes them: d may be z)
+    float x[VE];
+    unpack<T>(v[k], x);
+#pragma unroll
+    for (int e = 0; e < VE; ++e) x[e] = neg * exp_of(x[e], m);
+    T* at = d + sp.head + k * VE;
+    if (same) {
+      *reinterpret_cast<uint4*>(at) = pack<T>(x);
+    } else {
+#pragma unroll
+      for (int e = 0; e < VE; ++e) at[e] = from_f32<T>(x[e]);
+    }
+  }
+  if (edge >= 0) d[edge] = from_f32<T>(neg * exp_of(xe, m));
+  const int kt = target - sp.head;
+  if (kt >= 0 && kt < sp.full * VE ? (kt / VE) % THREADS == lane : edge == target) d[target] = from_f32<T>(coef * (1.f - exp_of(zy, m) / s));
+}
+
+// coef ([j = target] - exp(z_j - top) inv), inv null: 1, by workgroups of kThreads * kGradVectors vectors of a row; rows from the
+// last to the first: the last ones read are the likeliest to lie in a cache still
+constexpr int kGradVectors = 4;
+template <typename T>
+__global__ __launch_bounds__(kThreads) void grad_kernel(const T* logits, long stride, Rows of, const float* __restrict__ coefs,
+                                                        const float* __restrict__ tops, const float* __restrict__ invs, T* dlogits, long dstride,
+                                                        int parts, int rows) {
+  constexpr int VE = Span<T>::VE;
+  const int from_last = blockIdx.x / parts, row = rows - 1 - from_last, part = blockIdx.x - from_last * parts, lane = threadIdx.x;
+  const float coef = of.counts(row) ? coefs[row] : 0.f;
+  const T* z = logits + (long)row * stride;
+  T* d = dlogits + (long)row * dstride;
+  const bool same = (((uintptr_t)d ^ (uintptr_t)z) & 15) == 0;
+  const Span<T> sp(z, of.vocab);
+  const int k0 = part * kThreads * kGradVectors + lane, edge = part == 0 ? sp.edge(lane) : -1;
+  if (coef == 0.f) {
+#pragma unroll
+    for (int i = 0; i < kGradVectors; ++i) {
+      const int k = k0 + i * kThreads;
+      if (k >= sp.full) break;
+      T* at = d + sp.head + k * VE;
+      if (same) {
+        *reinterpret_cast<uint4*>(at) = make_uint4(0, 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int e = 0; e < VE; ++e) at[e] = from_f32<T>(0.f);
+      }
+    }
+    if (edge >= 0) d[edge] = from_f32<T>(0.f);
+    return;
+  }
+  const float top = tops[row], inv = invs ? invs[row] : 1.f, neg = -coef * inv;
+  const int target = of.targets[row];
+  const uint4* v = reinterpret_cast<const uint4*>(z + sp.head);
+  uint4 r[kGradVectors];
+#pragma unroll
+  for (int i = 0; i < kGradVectors; ++i) {
+    const int k = k0 + i * kThreads;
+    if (k < sp.full) r[i] = v[k];
+  }
+#pragma unroll
+  for (int i = 0; i < kGradVectors; ++i) {
+    const int k = k0 + i * kThreads, j = sp.head + k * VE;
+    if (k >= sp.full) break;
+    float x[VE];
+    unpack<T>(r[i], x);
+    const bool hot = target >= j && target < j + VE;
+    float y = 0.f;
+    if (hot) {
+#pragma unroll
+      for (int e = 0; e < VE; ++e) if (j + e == target) y = x[e];
+    }
+#pragma unroll
+    for (int e = 0; e < VE; ++e) x[e] = neg * exp_of(x[e], top);
+    T* at = d + j;
+    if (same) {
+      *reinterpret_cast<uint4*>(at) = pack<T>(x);
+    } else {
+#pragma unroll
+      for (int e = 0; e < VE; ++e) at[e] = from_f32<T>(x[e]);
+    }
+    if (hot) d[target] = from_f32<T>(coef * (1.f - exp_of(y, top) * inv));
+  }
+  if (edge >= 0) {
+    const float p = exp_of(to_f32(z[edge]), top) * inv;
+    d[edge] = from_f32<T>(edge == target ? coef * (1.f - p) : -coef * p);
+  }
 }
 
 // sum of n values in a fixed order, by one workgroup
@@ -139,35 +419,38 @@ __device__ __forceinline__ void sequence_rows(const int* offsets, int q, int row
   *a = x < 0 ? 0 : x > rows ? rows : x;
   *b = y < *a ? *a : y > rows ? rows : y;
 }
-__device__ __forceinline__ double neg_log_sigmoid(double y) { return fmax(-y, 0.0) + log1p(exp(-fabs(y))); }
 
 // One workgroup per pair: both sequences' sums of w (logp - ref), the pair's loss, and the coefficient of every row.
-__global__ __launch_bounds__(kThreads) void pair_kernel(PairArgs a, Rows of, int rows,
-                                                        const float* __restrict__ logp, float* __restrict__ rewards,
+__global__ __launch_bounds__(kThreads) void pair_kernel(PairArgs a, Rows of, int rows, const double* __restrict__ logp, float* __restrict__ rewards,
                                                         float* __restrict__ coef, double* __restrict__ part) {
-  __shared__ double red[2][kThreads];
+  __shared__ double red[2][kThreads / 64], slope_of;
   int lo[2], hi[2];
   for (int q = 0; q < 2; ++q) {
     sequence_rows(of.offsets, 2 * blockIdx.x + q, rows, &lo[q], &hi[q]);
     double acc = 0.0;
     for (int r = lo[q] + threadIdx.x; r < hi[q]; r += kThreads)
-      if (of.counts(r)) acc += of.weight_of(r) * ((double)logp[r] - (double)a.ref_logp[r]);
-    red[q][threadIdx.x] = acc;
+      if (of.counts(r)) acc += of.weight_of(r) * (logp[r] - (double)a.ref_logp[r]);
+    acc = wave_sum(acc);
+    if ((threadIdx.x & 63) == 0) red[q][threadIdx.x >> 6] = acc;
   }
   __syncthreads();
-  for (int o = kThreads / 2; o > 0; o >>= 1) {
-    if ((int)threadIdx.x < o) { red[0][threadIdx.x] += red[0][threadIdx.x + o]; red[1][threadIdx.x] += red[1][threadIdx.x + o]; }
-    __syncthreads();
-  }
-  const double sc = red[0][0], sr = red[1][0], x = a.beta * (sc - sr);
   if (threadIdx.x == 0) {
-    if (rewards) { rewards[2 * blockIdx.x] = (float)(a.beta * sc); rewards[2 * blockIdx.x + 1] = (float)(a.beta * sr); }
-    part[blockIdx.x] = a.scale * ((1.0 - a.smoothing) * neg_log_sigmoid(x) + a.smoothing * neg_log_sigmoid(-x));
+    double s[2];
+    for (int q = 0; q < 2; ++q) {
+      s[q] = red[q][0];
+      for (int w = 1; w < kThreads / 64; ++w) s[q] += red[q][w];
+      if (rewards) rewards[2 * blockIdx.x + q] = (float)(a.beta * s[q]);
+    }
+    const double x = a.beta * (s[0] - s[1]), e = exp(-fabs(x)), l = log1p(e);  // -log sigma(x) = max(-x, 0) + l
+    part[blockIdx.x] = a.scale * ((1.0 - a.smoothing) * (fmax(-x, 0.0) + l) + a.smoothing * (fmax(x, 0.0) + l));
+    const double above = x >= 0 ? 1.0 / (1.0 + e) : e / (1.0 + e);  // sigma(x)
+    const double below = x >= 0 ? e / (1.0 + e) : 1.0 / (1.0 + e);  // sigma(-x)
+    slope_of = a.scale * a.beta * (a.smoothing * above - (1.0 - a.smoothing) * below);
   }
-  const double slope = a.scale * a.beta * (a.smoothing / (1.0 + exp(-x)) - (1.0 - a.smoothing) / (1.0 + exp(x)));
+  __syncthreads();
+  const double slope = slope_of;
   for (int q = 0; q < 2; ++q)
-    for (int r = lo[q] + threadIdx.x; r < hi[q]; r += kThreads)
-      coef[r] = (float)((q ? -slope : slope) * of.weight_of(r));
+    for (int r = lo[q] + threadIdx.x; r < hi[q]; r += kThreads) coef[r] = (float)((q ? -slope : slope) * of.weight_of(r));
 }
 
 __global__ __launch_bounds__(kThreads) void fill_zero_kernel(float* p, int n) {
@@ -190,36 +473,60 @@ bool valid_dlogits(const zb_logits* x, const void* d, int64_t* stride) {
 }
 bool misaligned(const void* p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
 
-struct Workspace {  // rows: one partial loss, lse, log-probability and coefficient each
-  double* part;
-  float *lse, *logp, *coef;
+struct Workspace {  // rows: a partial loss, the log-probability, what makes probabilities of logits, the coefficient
+  double *part, *logp;
+  float *top, *inv, *coef;
 };
 size_t workspace_bytes(int rows, int pairs) {
   const size_t n = (size_t)(rows > pairs ? rows : pairs);
-  return n * sizeof(double) + 3 * (size_t)rows * sizeof(float) + 256;
+  return n * sizeof(double) + (size_t)rows * (sizeof(double) + 3 * sizeof(float)) + 256;
 }
 Workspace carve(void* base, int rows, int pairs) {
   Workspace w;
   w.part = (double*)base;
-  w.lse = (float*)(w.part + (rows > pairs ? rows : pairs));
-  w.logp = w.lse + rows;
-  w.coef = w.logp + rows;
+  w.logp = w.part + (rows > pairs ? rows : pairs);
+  w.top = (float*)(w.logp + rows);
+  w.inv = w.top + rows;
+  w.coef = w.inv + rows;
   return w;
 }
 
-#define ZB_BY_TYPE(x, call)                                     \
-  do {                                                          \
-    if ((x)->dtype == ZB_BF16) { using T = bf16_t; call; }      \
-    else { using T = float; call; }                             \
-  } while (0)
-
-void launch_logp(const zb_logits* x, const Rows& of, float* logp, float* lse, hipStream_t s) {
-  ZB_BY_TYPE(x, (row_logp_kernel<T><<<x->rows, kThreads, 0, s>>>((const T*)x->logits, x->row_stride, of, logp, lse)));
+template <typename T, bool POLICY>
+hipError_t launch_rows(const zb_logits* x, const Rows& of, const RowOut& out, const PolicyArgs& pol, void* dlogits, int64_t dstride, hipStream_t s) {
+  const int vectors = x->vocab / Span<T>::VE;  // at most: a row's start may leave one fewer
+#define ZB_ROWS(THREADS, NV)                                                                                                          \
+  if (vectors <= THREADS * NV) {                                                                                                      \
+    row_kernel<T, THREADS, NV, POLICY><<<x->rows, THREADS, 0, s>>>((const T*)x->logits, x->row_stride, of, out, pol, (T*)dlogits, dstride); \
+    return hipGetLastError();                                                                                                         \
+  }
+  ZB_ROWS(64, 2)
+  ZB_ROWS(256, 2)
+  ZB_ROWS(256, 4)
+  ZB_ROWS(512, 4)
+  ZB_ROWS(512, 8)
+  ZB_ROWS(1024, 7)
+  ZB_ROWS(1024, 10)
+  ZB_ROWS(1024, 16)
+#undef ZB_ROWS
+  long_row_kernel<T, POLICY><<<x->rows, 1024, 0, s>>>((const T*)x->logits, x->row_stride, of, out, pol, (T*)dlogits, dstride);
+  return hipGetLastError();
 }
-void launch_grad(const zb_logits* x, const Rows& of, const float* lse, const float* coef, void* d, int64_t stride, hipStream_t s) {
-  ZB_BY_TYPE(x, (row_grad_kernel<T><<<x->rows, kThreads, 0, s>>>((const T*)x->logits, x->row_stride, of, lse, coef, (T*)d, stride)));
+template <bool POLICY>
+hipError_t launch_rows(const zb_logits* x, const Rows& of, const RowOut& out, const PolicyArgs& pol, void* dlogits, int64_t dstride, hipStream_t s) {
+  return x->dtype == ZB_BF16 ? launch_rows<bf16_t, POLICY>(x, of, out, pol, dlogits, dstride, s)
+                             : launch_rows<float, POLICY>(x, of, out, pol, dlogits, dstride, s);
 }
-zb_status launched() { return hipGetLastError() == hipSuccess ? ZB_OK : ZB_EDEVICE; }
+template <typename T>
+hipError_t launch_grad(const zb_logits* x, const Rows& of, const float* coef, const float* top, const float* inv, void* d, int64_t stride, hipStream_t s) {
+  const int per = kThreads * kGradVectors, vectors = x->vocab / Span<T>::VE, parts = vectors > per ? (vectors + per - 1) / per : 1;
+  grad_kernel<T><<<(unsigned)x->rows * (unsigned)parts, kThreads, 0, s>>>((const T*)x->logits, x->row_stride, of, coef, top, inv, (T*)d, stride, parts,
+                                                                         x->rows);
+  return hipGetLastError();
+}
+hipError_t launch_grad(const zb_logits* x, const Rows& of, const float* coef, const float* top, const float* inv, void* d, int64_t stride, hipStream_t s) {
+  return x->dtype == ZB_BF16 ? launch_grad<bf16_t>(x, of, coef, top, inv, d, stride, s) : launch_grad<float>(x, of, coef, top, inv, d, stride, s);
+}
+zb_status said(hipError_t e) { return e == hipSuccess ? ZB_OK : ZB_EDEVICE; }
 
 }  // namespace
 }  // namespace zb
@@ -233,8 +540,7 @@ zb_status zb_token_logprobs(const zb_logits* x, float* logp, float* lse, void* h
   if (x->rows == 0) return ZB_OK;
   OnDeviceOf on((hipStream_t)hip_stream);
   if (!on.ok) return ZB_EDEVICE;
-  launch_logp(x, Rows{x->targets, nullptr, nullptr, 0, x->vocab}, logp, lse, (hipStream_t)hip_stream);
-  return launched();
+  return said(launch_rows<false>(x, Rows{x->targets, nullptr, nullptr, 0, x->vocab}, RowOut{logp, lse}, PolicyArgs{}, nullptr, 0, (hipStream_t)hip_stream));
 }
 
 zb_status zb_token_logprobs_backward(const zb_logits* x, const float* lse, const float* dlogp, void* dlogits, int64_t dlogits_stride,
@@ -244,8 +550,7 @@ zb_status zb_token_logprobs_backward(const zb_logits* x, const float* lse, const
   if (!lse || !dlogp || !dlogits) return ZB_EINVAL;
   OnDeviceOf on((hipStream_t)hip_stream);
   if (!on.ok) return ZB_EDEVICE;
-  launch_grad(x, Rows{x->targets, nullptr, nullptr, 0, x->vocab}, lse, dlogp, dlogits, dlogits_stride, (hipStream_t)hip_stream);
-  return launched();
+  return said(launch_grad(x, Rows{x->targets, nullptr, nullptr, 0, x->vocab}, dlogp, lse, nullptr, dlogits, dlogits_stride, (hipStream_t)hip_stream));
 }
 
 zb_status zb_loss_workspace_bytes(int32_t rows, int32_t pairs, size_t* bytes) {
@@ -272,13 +577,13 @@ zb_status zb_policy_loss(const zb_logits* x, const zb_policy* p, float* loss, fl
   if (x->rows) {
     const Rows of{x->targets, p->weight, nullptr, 0, x->vocab};
     const PolicyArgs a{p->old_logp, p->ref_logp, p->advantage, 1.0 - p->clip_low, 1.0 + p->clip_high, p->kl_coef, p->scale};
-    float* lp = logp ? logp : w.logp;
-    launch_logp(x, of, lp, w.lse, s);
-    policy_coef_kernel<<<(x->rows + kThreads - 1) / kThreads, kThreads, 0, s>>>(a, of, x->rows, lp, w.coef, w.part);
-    if (dlogits) launch_grad(x, of, w.lse, w.coef, dlogits, dlogits_stride, s);
+    RowOut out{logp};
+    out.part = w.part;
+    const hipError_t e = launch_rows<true>(x, of, out, a, dlogits, dlogits_stride, s);
+    if (e != hipSuccess) return ZB_EDEVICE;
   }
   sum_kernel<<<1, kThreads, 0, s>>>(w.part, x->rows, loss);
-  return launched();
+  return said(hipGetLastError());
 }
 
 zb_status zb_preference_loss(const zb_logits* x, const zb_preference* p, float* loss, float* logp, float* rewards, void* dlogits,
@@ -295,19 +600,21 @@ zb_status zb_preference_loss(const zb_logits* x, const zb_preference* p, float* 
   OnDeviceOf on(s);
   if (!on.ok) return ZB_EDEVICE;
   const Workspace w = carve(workspace, x->rows, p->pairs);
-  float* lp = logp ? logp : w.logp;
   const Rows of{x->targets, p->weight, p->pairs ? p->offsets : nullptr, p->pairs ? 2 * p->pairs : -1, x->vocab};
   if (x->rows) {
+    RowOut out{logp};
+    out.top = w.top; out.inv = w.inv; out.logp64 = w.logp;
     fill_zero_kernel<<<(x->rows + kThreads - 1) / kThreads, kThreads, 0, s>>>(w.coef, x->rows);
-    launch_logp(x, of, lp, w.lse, s);
+    if (hipGetLastError() != hipSuccess || launch_rows<false>(x, of, out, PolicyArgs{}, nullptr, 0, s) != hipSuccess) return ZB_EDEVICE;
   }
   if (p->pairs) {
     const PairArgs a{p->ref_logp, p->beta, p->label_smoothing, p->scale};
-    pair_kernel<<<p->pairs, kThreads, 0, s>>>(a, of, x->rows, lp, rewards, w.coef, w.part);
+    pair_kernel<<<p->pairs, kThreads, 0, s>>>(a, of, x->rows, w.logp, rewards, w.coef, w.part);
+    if (hipGetLastError() != hipSuccess) return ZB_EDEVICE;
   }
-  if (x->rows && dlogits) launch_grad(x, of, w.lse, w.coef, dlogits, dlogits_stride, s);
+  if (x->rows && dlogits && launch_grad(x, of, w.coef, w.top, w.inv, dlogits, dlogits_stride, s) != hipSuccess) return ZB_EDEVICE;
   sum_kernel<<<1, kThreads, 0, s>>>(w.part, p->pairs, loss);
-  return launched();
+  return said(hipGetLastError());
 }
 
 }  // extern "C"
