@@ -105,41 +105,112 @@ template <int N> __device__ __forceinline__ float block_sum(float v, float* red)
   return v;
 }
 
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+// NT: the caches are told that the line is not needed again
+template <bool NT> __device__ __forceinline__ uint4 get16(const uint4* at) {
+  if (!NT) return *at;
+  const u32x4 t = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(at));
+  return make_uint4(t.x, t.y, t.z, t.w);
+}
+template <bool NT> __device__ __forceinline__ void put16(void* at, const uint4& v) {
+  const u32x4 t = {v.x, v.y, v.z, v.w};
+  if (NT) __builtin_nontemporal_store(t, reinterpret_cast<u32x4*>(at));
+  else *reinterpret_cast<u32x4*>(at) = t;
+}
+
 // zeros in a row's gradient, by THREADS lanes
-template <typename T> __device__ __forceinline__ void clear_row(T* d, int vocab, int threads) {
+template <typename T, bool NT> __device__ __forceinline__ void clear_row(T* d, int vocab, int threads) {
   const Span<T> sp(d, vocab);
   const int lane = threadIdx.x;
   uint4* v = reinterpret_cast<uint4*>(d + sp.head);
-  for (int k = lane; k < sp.full; k += threads) v[k] = make_uint4(0, 0, 0, 0);
+  for (int k = lane; k < sp.full; k += threads) put16<NT>(v + k, make_uint4(0, 0, 0, 0));
   const int e = sp.edge(lane);
   if (e >= 0) d[e] = from_f32<T>(0.f);
 }
 
 struct PolicyArgs {
   const float *old_logp, *ref_logp, *advantage;
-  double lo, hi, kl, scale;
+  double lo, hi, log_lo, log_hi, kl, scale;  // borders of the ratio and of its logarithm
 };
-// loss of a row and its derivative by the row's log-probability
+// exp(d) to the last bit or two of fp32, whatever the size of d
+__device__ __forceinline__ double exp_near(double d) {
+  const float h = (float)d, l = (float)(d - (double)h);
+  const float e = expf(h);
+  return (double)e + (e < INFINITY ? (double)(e * l) : 0.0);
+}
+// exp(d) - d - 1; the digits that the subtraction would take near 0 come from the series
+__device__ __forceinline__ double exp_above_line(double d) {
+  if (fabs(d) > 1.0) return exp_near(d) - d - 1.0;
+  const float x = (float)d;
+  float t = 1.0f / 39916800.0f;  // 1 / 11!
+  t = fmaf(t, x, 1.0f / 3628800.0f); t = fmaf(t, x, 1.0f / 362880.0f); t = fmaf(t, x, 1.0f / 40320.0f); t = fmaf(t, x, 1.0f / 5040.0f);
+  t = fmaf(t, x, 1.0f / 720.0f); t = fmaf(t, x, 1.0f / 120.0f); t = fmaf(t, x, 1.0f / 24.0f); t = fmaf(t, x, 1.0f / 6.0f);
+  t = fmaf(t, x, 0.5f);
+  return d * d * (double)t;
+}
+// Loss of a row and its derivative by the row's log-probability.  One lane does this while the others wait, so it takes the
+// exponential of fp32; what is compared with a border is the logarithm, in 64 bits.
 __device__ __forceinline__ double policy_row(const PolicyArgs& a, const Rows& of, int row, double logp, double* slope) {
-  const double adv = a.advantage[row], rho = exp(logp - (double)a.old_logp[row]);
-  const double w = of.weight_of(row) * a.scale;
-  const double held = rho < a.lo ? a.lo : rho > a.hi ? a.hi : rho;
+  const double adv = a.advantage[row], x = logp - (double)a.old_logp[row], rho = exp_near(x), w = of.weight_of(row) * a.scale;
+  const bool above = x > a.log_hi, below = x < a.log_lo;
+  const double held = above ? a.hi : below ? a.lo : rho;
   double loss = -fmin(rho * adv, held * adv);
-  double g = (adv > 0 && rho > a.hi) || (adv < 0 && rho < a.lo) ? 0.0 : -adv * rho;
+  double g = (adv > 0 && above) || (adv < 0 && below) ? 0.0 : -adv * rho;
   if (a.kl != 0.0) {
-    const double d = (double)a.ref_logp[row] - logp, e = expm1(d);
-    loss += a.kl * (e - d);
-    g -= a.kl * e;
+    const double d = (double)a.ref_logp[row] - logp, k = exp_above_line(d);
+    loss += a.kl * k;
+    g -= a.kl * (k + d);
   }
   *slope = w * g;
   return w * loss;
+}
+
+// Sum of n values by the THREADS lanes of a workgroup, in an order that only n decides; lane 0 has it.
+template <int THREADS, class F> __device__ __forceinline__ double sum_of(int n, F&& value) {
+  __shared__ double red[THREADS / 64];
+  double acc = 0.0;
+  for (int i = threadIdx.x; i < n; i += THREADS) acc += value(i);
+  acc = wave_sum(acc);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = acc;
+  __syncthreads();
+  acc = red[0];
+#pragma unroll
+  for (int w = 1; w < THREADS / 64; ++w) acc += red[w];
+  return acc;
+}
+__global__ __launch_bounds__(1024) void sum_kernel(const double* __restrict__ part, int n, float* __restrict__ out) {
+  const double s = sum_of<1024>(n, [&](int i) { return part[i]; });
+  if (threadIdx.x == 0) *out = (float)s;
+}
+// A launch of up to kSumInPlace workgroups adds their partial losses itself: the workgroup that is through last does, reading past the
+// caches of the XCDs what the others wrote past them.  `done` counts modulo the workgroups, so it is 0 again for the next call.
+constexpr int kSumInPlace = 256;
+struct Total {
+  float* loss;     // null: a kernel of its own adds the partial losses
+  unsigned* done;
+};
+template <int THREADS> __device__ __forceinline__ void add_to_total(const Total& t, double* part, double mine) {  // mine: lane 0's
+  __shared__ bool last;
+  if (!t.loss) {
+    if (threadIdx.x == 0) part[blockIdx.x] = mine;
+    return;
+  }
+  if (threadIdx.x == 0) {
+    __hip_atomic_store(part + blockIdx.x, mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    last = __builtin_amdgcn_atomic_inc32(t.done, gridDim.x - 1, __ATOMIC_ACQ_REL, "agent") == gridDim.x - 1;
+  }
+  __syncthreads();
+  if (!last) return;
+  const double s = sum_of<THREADS>((int)gridDim.x, [&](int i) { return __hip_atomic_load(part + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); });
+  if (threadIdx.x == 0) *t.loss = (float)s;
 }
 
 struct RowOut {  // what the row kernels leave of a row; null: not wanted
   float *logp, *lse;
   float *top, *inv;  // p_j = exp(z_j - top) * inv
   double *logp64;    // logp before its rounding
-  double *part;      // with a policy: its loss
+  double* part;      // with a policy: its loss
+  Total total;
 };
 __device__ __forceinline__ void put_row(const RowOut& o, int row, double logp, double lse, float top, float s) {
   if (o.logp) o.logp[row] = (float)logp;
@@ -152,21 +223,20 @@ __device__ __forceinline__ void put_no_row(const RowOut& o, int row) {
   if (o.lse) o.lse[row] = 0.f;
   if (o.top) { o.top[row] = 0.f; o.inv[row] = 0.f; }
   if (o.logp64) o.logp64[row] = 0.0;
-  if (o.part) o.part[row] = 0.0;
 }
 
-// One workgroup per row, the row in registers (NV vectors a lane): read once for the maximum, the sum and, with POLICY, the
-// gradient that follows from the row's own log-probability.
-template <typename T, int THREADS, int NV, bool POLICY>
-__global__ __launch_bounds__(THREADS) void row_kernel(const T* logits, long stride, Rows of, RowOut out, PolicyArgs pol, T* dlogits, long dstride) {
+// The policy loss, one workgroup per row, the row in registers (NV vectors a lane): read once for the maximum, the sum and the
+// gradient, which follows from the row's own log-probability.
+template <typename T, int THREADS, int NV, bool NT>
+__device__ __forceinline__ double policy_in_registers(const T* logits, long stride, Rows of, RowOut out, PolicyArgs pol, T* dlogits, long dstride) {
   constexpr int VE = Span<T>::VE, N = THREADS / 64;
   __shared__ float red_m[N], red_s[N], coef_of;
   const int row = blockIdx.x, lane = threadIdx.x;
   T* d = dlogits + (long)row * dstride;
   if (!of.counts(row)) {
     if (lane == 0) put_no_row(out, row);
-    if (POLICY && dlogits) clear_row<T>(d, of.vocab, THREADS);
-    return;
+    if (dlogits) clear_row<T, NT>(d, of.vocab, THREADS);
+    return 0.0;
   }
   const T* z = logits + (long)row * stride;
   const Span<T> sp(z, of.vocab);
@@ -175,7 +245,7 @@ __global__ __launch_bounds__(THREADS) void row_kernel(const T* logits, long stri
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int k = i * THREADS + lane;
-    r[i] = k < sp.full ? v[k] : empty_pack<T>();
+    r[i] = k < sp.full ? get16<NT>(v + k) : empty_pack<T>();
   }
   const int edge = sp.edge(lane);
   const float xe = edge >= 0 ? to_f32(z[edge]) : -INFINITY;
@@ -200,26 +270,20 @@ __global__ __launch_bounds__(THREADS) void row_kernel(const T* logits, long stri
     for (int e = 0; e < VE; e += 2) { s0 += exp_of(x[e], m); s1 += exp_of(x[e + 1], m); }
   }
   const float s = block_sum<N>(s0 + s1, red_s);
-  if (!POLICY) {
-    if (lane == 0) {
-      const double l = log_of(s);
-      put_row(out, row, ((double)zy - (double)m) - l, (double)m + l, m, s);
-    }
-    return;
-  }
+  double loss = 0.0;
   if (lane == 0) {
     const double l = log_of(s), lp = ((double)zy - (double)m) - l;
     double slope;
-    out.part[row] = policy_row(pol, of, row, lp, &slope);
+    loss = policy_row(pol, of, row, lp, &slope);
     put_row(out, row, lp, (double)m + l, m, s);
     coef_of = (float)slope;
   }
-  if (!dlogits) return;
+  if (!dlogits) return loss;
   __syncthreads();
   const float coef = coef_of, neg = -coef / s;
   if (coef == 0.f) {
-    clear_row<T>(d, of.vocab, THREADS);
-    return;
+    clear_row<T, NT>(d, of.vocab, THREADS);
+    return loss;
   }
   const bool same = (((uintptr_t)d ^ (uintptr_t)z) & 15) == 0;
   as_loaded(r);
@@ -233,7 +297,7 @@ __global__ __launch_bounds__(THREADS) void row_kernel(const T* logits, long stri
     for (int e = 0; e < VE; ++e) x[e] = neg * exp_of(x[e], m);
     T* at = d + sp.head + k * VE;
     if (same) {
-      *reinterpret_cast<uint4*>(at) = pack<T>(x);
+      put16<NT>(at, pack<T>(x));
     } else {
 #pragma unroll
       for (int e = 0; e < VE; ++e) at[e] = from_f32<T>(x[e]);
@@ -243,19 +307,26 @@ __global__ __launch_bounds__(THREADS) void row_kernel(const T* logits, long stri
   // the lane that wrote the target's entry writes it again, whole
   const int kt = target - sp.head;
   if (kt >= 0 && kt < sp.full * VE ? (kt / VE) % THREADS == lane : edge == target) d[target] = from_f32<T>(coef * (1.f - exp_of(zy, m) / s));
+  return loss;
+}
+template <typename T, int THREADS, int NV, int WAVES, bool NT>
+__global__ __launch_bounds__(THREADS, WAVES) void policy_row_kernel(const T* logits, long stride, Rows of, RowOut out, PolicyArgs pol, T* dlogits,
+                                                                    long dstride) {
+  add_to_total<THREADS>(out.total, out.part, policy_in_registers<T, THREADS, NV, NT>(logits, stride, of, out, pol, dlogits, dstride));
 }
 
-// The same for rows that registers do not hold: read once for maximum and sum together, and again for the gradient.
-template <typename T, bool POLICY>
-__global__ __launch_bounds__(1024) void long_row_kernel(const T* logits, long stride, Rows of, RowOut out, PolicyArgs pol, T* dlogits, long dstride) {
-  constexpr int VE = Span<T>::VE, THREADS = 1024, N = THREADS / 64, U = 4;
+// lse and log-probability, one workgroup per row: maximum and sum in one pass, U vectors of a lane at a time.  With POLICY, for rows that
+// registers do not hold, the policy loss: the row is read again for the gradient.
+template <typename T, int THREADS, int U, bool POLICY, bool NT>
+__device__ __forceinline__ double row_in_passes(const T* logits, long stride, Rows of, RowOut out, PolicyArgs pol, T* dlogits, long dstride) {
+  constexpr int VE = Span<T>::VE, N = THREADS / 64;
   __shared__ float red_m[N], red_s[N], coef_of;
   const int row = blockIdx.x, lane = threadIdx.x;
   T* d = dlogits + (long)row * dstride;
   if (!of.counts(row)) {
     if (lane == 0) put_no_row(out, row);
-    if (POLICY && dlogits) clear_row<T>(d, of.vocab, THREADS);
-    return;
+    if (POLICY && dlogits) clear_row<T, NT>(d, of.vocab, THREADS);
+    return 0.0;
   }
   const T* z = logits + (long)row * stride;
   const Span<T> sp(z, of.vocab);
@@ -267,7 +338,7 @@ __global__ __launch_bounds__(1024) void long_row_kernel(const T* logits, long st
   for (int k0 = lane; k0 < sp.full; k0 += U * THREADS) {
     uint4 r[U];
 #pragma unroll
-    for (int i = 0; i < U; ++i) r[i] = k0 + i * THREADS < sp.full ? v[k0 + i * THREADS] : empty_pack<T>();
+    for (int i = 0; i < U; ++i) r[i] = k0 + i * THREADS < sp.full ? get16<NT>(v + k0 + i * THREADS) : empty_pack<T>();
     float top = mine;
 #pragma unroll
     for (int i = 0; i < U; ++i) {
@@ -292,31 +363,32 @@ __global__ __launch_bounds__(1024) void long_row_kernel(const T* logits, long st
   // lanes without a finite logit add nothing, unless they saw a NaN; a row without one is undefined
   const float own = mine == -INFINITY && m > -INFINITY ? (part != part ? part : 0.f) : part * exp_of(mine, m);
   const float s = block_sum<N>(own, red_s);
+  double loss = 0.0;
   if (lane == 0) {
     const double l = log_of(s), lp = ((double)zy - (double)m) - l;
     if (POLICY) {
       double slope;
-      out.part[row] = policy_row(pol, of, row, lp, &slope);
+      loss = policy_row(pol, of, row, lp, &slope);
       coef_of = (float)slope;
     }
     put_row(out, row, lp, (double)m + l, m, s);
   }
-  if (!POLICY || !dlogits) return;
+  if (!POLICY || !dlogits) return loss;
   __syncthreads();
   const float coef = coef_of, neg = -coef / s;
   if (coef == 0.f) {
-    clear_row<T>(d, of.vocab, THREADS);
-    return;
+    clear_row<T, NT>(d, of.vocab, THREADS);
+    return loss;
   }
   const bool same = (((uintptr_t)d ^ (uintptr_t)z) & 15) == 0;
   for (int k = lane; k < sp.full; k += THREADS) {  // (a lane reads its entries before it writes them: d may be z)
     float x[VE];
-    unpack<T>(v[k], x);
+    unpack<T>(get16<NT>(v + k), x);
 #pragma unroll
     for (int e = 0; e < VE; ++e) x[e] = neg * exp_of(x[e], m);
     T* at = d + sp.head + k * VE;
     if (same) {
-      *reinterpret_cast<uint4*>(at) = pack<T>(x);
+      put16<NT>(at, pack<T>(x));
     } else {
 #pragma unroll
       for (int e = 0; e < VE; ++e) at[e] = from_f32<T>(x[e]);
@@ -325,12 +397,18 @@ __global__ __launch_bounds__(1024) void long_row_kernel(const T* logits, long st
   if (edge >= 0) d[edge] = from_f32<T>(neg * exp_of(xe, m));
   const int kt = target - sp.head;
   if (kt >= 0 && kt < sp.full * VE ? (kt / VE) % THREADS == lane : edge == target) d[target] = from_f32<T>(coef * (1.f - exp_of(zy, m) / s));
+  return loss;
+}
+template <typename T, int THREADS, int U, bool POLICY, bool NT>
+__global__ __launch_bounds__(THREADS) void row_kernel(const T* logits, long stride, Rows of, RowOut out, PolicyArgs pol, T* dlogits, long dstride) {
+  const double loss = row_in_passes<T, THREADS, U, POLICY, NT>(logits, stride, of, out, pol, dlogits, dstride);
+  if (POLICY) add_to_total<THREADS>(out.total, out.part, loss);
 }
 
 // coef ([j = target] - exp(z_j - top) inv), inv null: 1, by workgroups of kThreads * kGradVectors vectors of a row; rows from the
 // last to the first: the last ones read are the likeliest to lie in a cache still
 constexpr int kGradVectors = 4;
-template <typename T>
+template <typename T, bool NT>
 __global__ __launch_bounds__(kThreads) void grad_kernel(const T* logits, long stride, Rows of, const float* __restrict__ coefs,
                                                         const float* __restrict__ tops, const float* __restrict__ invs, T* dlogits, long dstride,
                                                         int parts, int rows) {
@@ -349,7 +427,7 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(const T* logits, long st
       if (k >= sp.full) break;
       T* at = d + sp.head + k * VE;
       if (same) {
-        *reinterpret_cast<uint4*>(at) = make_uint4(0, 0, 0, 0);
+        put16<NT>(at, make_uint4(0, 0, 0, 0));
       } else {
 #pragma unroll
         for (int e = 0; e < VE; ++e) at[e] = from_f32<T>(0.f);
@@ -365,7 +443,7 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(const T* logits, long st
 #pragma unroll
   for (int i = 0; i < kGradVectors; ++i) {
     const int k = k0 + i * kThreads;
-    if (k < sp.full) r[i] = v[k];
+    if (k < sp.full) r[i] = get16<NT>(v + k);
   }
 #pragma unroll
   for (int i = 0; i < kGradVectors; ++i) {
@@ -383,7 +461,7 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(const T* logits, long st
     for (int e = 0; e < VE; ++e) x[e] = neg * exp_of(x[e], top);
     T* at = d + j;
     if (same) {
-      *reinterpret_cast<uint4*>(at) = pack<T>(x);
+      put16<NT>(at, pack<T>(x));
     } else {
 #pragma unroll
       for (int e = 0; e < VE; ++e) at[e] = from_f32<T>(x[e]);
@@ -394,20 +472,6 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(const T* logits, long st
     const float p = exp_of(to_f32(z[edge]), top) * inv;
     d[edge] = from_f32<T>(edge == target ? coef * (1.f - p) : -coef * p);
   }
-}
-
-// sum of n values in a fixed order, by one workgroup
-__global__ __launch_bounds__(kThreads) void sum_kernel(const double* __restrict__ part, int n, float* __restrict__ out) {
-  __shared__ double red[kThreads];
-  double acc = 0.0;
-  for (int i = threadIdx.x; i < n; i += kThreads) acc += part[i];
-  red[threadIdx.x] = acc;
-  __syncthreads();
-  for (int o = kThreads / 2; o > 0; o >>= 1) {
-    if ((int)threadIdx.x < o) red[threadIdx.x] += red[threadIdx.x + o];
-    __syncthreads();
-  }
-  if (threadIdx.x == 0) *out = (float)red[0];
 }
 
 struct PairArgs {
@@ -422,7 +486,7 @@ __device__ __forceinline__ void sequence_rows(const int* offsets, int q, int row
 
 // One workgroup per pair: both sequences' sums of w (logp - ref), the pair's loss, and the coefficient of every row.
 __global__ __launch_bounds__(kThreads) void pair_kernel(PairArgs a, Rows of, int rows, const double* __restrict__ logp, float* __restrict__ rewards,
-                                                        float* __restrict__ coef, double* __restrict__ part) {
+                                                        float* __restrict__ coef, double* part, Total total) {
   __shared__ double red[2][kThreads / 64], slope_of;
   int lo[2], hi[2];
   for (int q = 0; q < 2; ++q) {
@@ -434,6 +498,7 @@ __global__ __launch_bounds__(kThreads) void pair_kernel(PairArgs a, Rows of, int
     if ((threadIdx.x & 63) == 0) red[q][threadIdx.x >> 6] = acc;
   }
   __syncthreads();
+  double loss = 0.0;
   if (threadIdx.x == 0) {
     double s[2];
     for (int q = 0; q < 2; ++q) {
@@ -442,7 +507,7 @@ __global__ __launch_bounds__(kThreads) void pair_kernel(PairArgs a, Rows of, int
       if (rewards) rewards[2 * blockIdx.x + q] = (float)(a.beta * s[q]);
     }
     const double x = a.beta * (s[0] - s[1]), e = exp(-fabs(x)), l = log1p(e);  // -log sigma(x) = max(-x, 0) + l
-    part[blockIdx.x] = a.scale * ((1.0 - a.smoothing) * (fmax(-x, 0.0) + l) + a.smoothing * (fmax(x, 0.0) + l));
+    loss = a.scale * ((1.0 - a.smoothing) * (fmax(-x, 0.0) + l) + a.smoothing * (fmax(x, 0.0) + l));
     const double above = x >= 0 ? 1.0 / (1.0 + e) : e / (1.0 + e);  // sigma(x)
     const double below = x >= 0 ? e / (1.0 + e) : 1.0 / (1.0 + e);  // sigma(-x)
     slope_of = a.scale * a.beta * (a.smoothing * above - (1.0 - a.smoothing) * below);
@@ -451,11 +516,7 @@ __global__ __launch_bounds__(kThreads) void pair_kernel(PairArgs a, Rows of, int
   const double slope = slope_of;
   for (int q = 0; q < 2; ++q)
     for (int r = lo[q] + threadIdx.x; r < hi[q]; r += kThreads) coef[r] = (float)((q ? -slope : slope) * of.weight_of(r));
-}
-
-__global__ __launch_bounds__(kThreads) void fill_zero_kernel(float* p, int n) {
-  const int i = blockIdx.x * kThreads + threadIdx.x;
-  if (i < n) p[i] = 0.f;
+  add_to_total<kThreads>(total, part, loss);
 }
 
 constexpr int kMaxRows = 1 << 24;
@@ -473,7 +534,8 @@ bool valid_dlogits(const zb_logits* x, const void* d, int64_t* stride) {
 }
 bool misaligned(const void* p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
 
-struct Workspace {  // rows: a partial loss, the log-probability, what makes probabilities of logits, the coefficient
+struct Workspace {  // a counter; per row a partial loss, the log-probability, what makes probabilities of logits, the coefficient
+  unsigned* done;
   double *part, *logp;
   float *top, *inv, *coef;
 };
@@ -483,7 +545,8 @@ size_t workspace_bytes(int rows, int pairs) {
 }
 Workspace carve(void* base, int rows, int pairs) {
   Workspace w;
-  w.part = (double*)base;
+  w.done = (unsigned*)base;
+  w.part = (double*)((char*)base + 64);
   w.logp = w.part + (rows > pairs ? rows : pairs);
   w.top = (float*)(w.logp + rows);
   w.inv = w.top + rows;
@@ -491,36 +554,57 @@ Workspace carve(void* base, int rows, int pairs) {
   return w;
 }
 
-template <typename T, bool POLICY>
-hipError_t launch_rows(const zb_logits* x, const Rows& of, const RowOut& out, const PolicyArgs& pol, void* dlogits, int64_t dstride, hipStream_t s) {
-  const int vectors = x->vocab / Span<T>::VE;  // at most: a row's start may leave one fewer
-#define ZB_ROWS(THREADS, NV)                                                                                                          \
-  if (vectors <= THREADS * NV) {                                                                                                      \
-    row_kernel<T, THREADS, NV, POLICY><<<x->rows, THREADS, 0, s>>>((const T*)x->logits, x->row_stride, of, out, pol, (T*)dlogits, dstride); \
-    return hipGetLastError();                                                                                                         \
-  }
-  ZB_ROWS(64, 2)
-  ZB_ROWS(256, 2)
-  ZB_ROWS(256, 4)
-  ZB_ROWS(512, 4)
-  ZB_ROWS(512, 8)
-  ZB_ROWS(1024, 7)
-  ZB_ROWS(1024, 10)
-  ZB_ROWS(1024, 16)
+// Lines that no cache would hold until they are wanted again: logits of over 64 MB, a quarter of the last cache (the gradient and
+// what comes next want their place in it too).  us with / without: log-probabilities of 4096 x 50432 bf16 69 / 74, policy loss of the same
+// 149 / 161; 64 x 50432, read from the caches, 9.3 / 7.4 and 12.1 / 9.7.
+bool past_caches(const zb_logits* x) { return (size_t)x->rows * x->vocab * (x->dtype == ZB_BF16 ? 2 : 4) > (size_t)64 << 20; }
+
+#define ZB_NT(call)                                                          \
+  do {                                                                       \
+    if (past_caches(x)) { constexpr bool NT = true; call; }                  \
+    else { constexpr bool NT = false; call; }                                \
+  } while (0)
+
+template <typename T> hipError_t launch_logp(const zb_logits* x, const Rows& of, const RowOut& out, hipStream_t s) {
+  const int vectors = x->vocab / Span<T>::VE;
+#define ZB_ROWS(THREADS, U)                                                                                                                   \
+  ZB_NT((row_kernel<T, THREADS, U, false, NT><<<x->rows, THREADS, 0, s>>>((const T*)x->logits, x->row_stride, of, out, PolicyArgs{}, (T*)nullptr, 0)))
+  if (vectors <= 512) ZB_ROWS(64, 4);
+  else if (vectors <= 2048) ZB_ROWS(256, 4);
+  else if (x->rows >= 512) ZB_ROWS(512, 4);
+  else ZB_ROWS(1024, 2);
 #undef ZB_ROWS
-  long_row_kernel<T, POLICY><<<x->rows, 1024, 0, s>>>((const T*)x->logits, x->row_stride, of, out, pol, (T*)dlogits, dstride);
   return hipGetLastError();
 }
-template <bool POLICY>
-hipError_t launch_rows(const zb_logits* x, const Rows& of, const RowOut& out, const PolicyArgs& pol, void* dlogits, int64_t dstride, hipStream_t s) {
-  return x->dtype == ZB_BF16 ? launch_rows<bf16_t, POLICY>(x, of, out, pol, dlogits, dstride, s)
-                             : launch_rows<float, POLICY>(x, of, out, pol, dlogits, dstride, s);
+hipError_t launch_logp(const zb_logits* x, const Rows& of, const RowOut& out, hipStream_t s) {
+  return x->dtype == ZB_BF16 ? launch_logp<bf16_t>(x, of, out, s) : launch_logp<float>(x, of, out, s);
+}
+
+template <typename T>
+hipError_t launch_policy(const zb_logits* x, const Rows& of, const RowOut& out, const PolicyArgs& pol, void* dlogits, int64_t dstride, hipStream_t s) {
+  const int vectors = x->vocab / Span<T>::VE;  // at most: a row's start may leave one fewer
+#define ZB_ROWS(THREADS, NV, WAVES)                                                                                                              \
+  if (vectors <= THREADS * NV) {                                                                                                                 \
+    ZB_NT((policy_row_kernel<T, THREADS, NV, WAVES, NT><<<x->rows, THREADS, 0, s>>>((const T*)x->logits, x->row_stride, of, out, pol, (T*)dlogits, \
+                                                                                   dstride)));                                                   \
+    return hipGetLastError();                                                                                                                    \
+  }
+  ZB_ROWS(64, 4, 1)
+  ZB_ROWS(256, 4, 1)
+  ZB_ROWS(512, 4, 1)
+  ZB_ROWS(512, 8, 6)
+  ZB_ROWS(1024, 7, 8)
+  ZB_ROWS(512, 16, 4)
+  ZB_ROWS(512, 25, 4)
+#undef ZB_ROWS
+  ZB_NT((row_kernel<T, 1024, 4, true, NT><<<x->rows, 1024, 0, s>>>((const T*)x->logits, x->row_stride, of, out, pol, (T*)dlogits, dstride)));
+  return hipGetLastError();
 }
 template <typename T>
 hipError_t launch_grad(const zb_logits* x, const Rows& of, const float* coef, const float* top, const float* inv, void* d, int64_t stride, hipStream_t s) {
   const int per = kThreads * kGradVectors, vectors = x->vocab / Span<T>::VE, parts = vectors > per ? (vectors + per - 1) / per : 1;
-  grad_kernel<T><<<(unsigned)x->rows * (unsigned)parts, kThreads, 0, s>>>((const T*)x->logits, x->row_stride, of, coef, top, inv, (T*)d, stride, parts,
-                                                                         x->rows);
+  ZB_NT((grad_kernel<T, NT><<<(unsigned)x->rows * (unsigned)parts, kThreads, 0, s>>>((const T*)x->logits, x->row_stride, of, coef, top, inv, (T*)d,
+                                                                                     stride, parts, x->rows)));
   return hipGetLastError();
 }
 hipError_t launch_grad(const zb_logits* x, const Rows& of, const float* coef, const float* top, const float* inv, void* d, int64_t stride, hipStream_t s) {
@@ -540,7 +624,7 @@ zb_status zb_token_logprobs(const zb_logits* x, float* logp, float* lse, void* h
   if (x->rows == 0) return ZB_OK;
   OnDeviceOf on((hipStream_t)hip_stream);
   if (!on.ok) return ZB_EDEVICE;
-  return said(launch_rows<false>(x, Rows{x->targets, nullptr, nullptr, 0, x->vocab}, RowOut{logp, lse}, PolicyArgs{}, nullptr, 0, (hipStream_t)hip_stream));
+  return said(launch_logp(x, Rows{x->targets, nullptr, nullptr, 0, x->vocab}, RowOut{logp, lse}, (hipStream_t)hip_stream));
 }
 
 zb_status zb_token_logprobs_backward(const zb_logits* x, const float* lse, const float* dlogp, void* dlogits, int64_t dlogits_stride,
@@ -576,13 +660,15 @@ zb_status zb_policy_loss(const zb_logits* x, const zb_policy* p, float* loss, fl
   const Workspace w = carve(workspace, x->rows, 0);
   if (x->rows) {
     const Rows of{x->targets, p->weight, nullptr, 0, x->vocab};
-    const PolicyArgs a{p->old_logp, p->ref_logp, p->advantage, 1.0 - p->clip_low, 1.0 + p->clip_high, p->kl_coef, p->scale};
+    const PolicyArgs a{p->old_logp, p->ref_logp, p->advantage, 1.0 - p->clip_low, 1.0 + p->clip_high, log(1.0 - p->clip_low), log1p(p->clip_high), p->kl_coef, p->scale};
     RowOut out{logp};
     out.part = w.part;
-    const hipError_t e = launch_rows<true>(x, of, out, a, dlogits, dlogits_stride, s);
-    if (e != hipSuccess) return ZB_EDEVICE;
+    if (x->rows <= kSumInPlace) out.total = Total{loss, w.done};
+    const hipError_t e = x->dtype == ZB_BF16 ? launch_policy<bf16_t>(x, of, out, a, dlogits, dlogits_stride, s)
+                                             : launch_policy<float>(x, of, out, a, dlogits, dlogits_stride, s);
+    if (e != hipSuccess || out.total.loss) return said(e);
   }
-  sum_kernel<<<1, kThreads, 0, s>>>(w.part, x->rows, loss);
+  sum_kernel<<<1, 1024, 0, s>>>(w.part, x->rows, loss);
   return said(hipGetLastError());
 }
 
@@ -604,16 +690,15 @@ zb_status zb_preference_loss(const zb_logits* x, const zb_preference* p, float* 
   if (x->rows) {
     RowOut out{logp};
     out.top = w.top; out.inv = w.inv; out.logp64 = w.logp;
-    fill_zero_kernel<<<(x->rows + kThreads - 1) / kThreads, kThreads, 0, s>>>(w.coef, x->rows);
-    if (hipGetLastError() != hipSuccess || launch_rows<false>(x, of, out, PolicyArgs{}, nullptr, 0, s) != hipSuccess) return ZB_EDEVICE;
+    if (launch_logp(x, of, out, s) != hipSuccess) return ZB_EDEVICE;
   }
   if (p->pairs) {
     const PairArgs a{p->ref_logp, p->beta, p->label_smoothing, p->scale};
-    pair_kernel<<<p->pairs, kThreads, 0, s>>>(a, of, x->rows, w.logp, rewards, w.coef, w.part);
+    pair_kernel<<<p->pairs, kThreads, 0, s>>>(a, of, x->rows, w.logp, rewards, w.coef, w.part, p->pairs <= kSumInPlace ? Total{loss, w.done} : Total{});
     if (hipGetLastError() != hipSuccess) return ZB_EDEVICE;
   }
   if (x->rows && dlogits && launch_grad(x, of, w.coef, w.top, w.inv, dlogits, dlogits_stride, s) != hipSuccess) return ZB_EDEVICE;
-  sum_kernel<<<1, kThreads, 0, s>>>(w.part, p->pairs, loss);
+  if (!p->pairs || p->pairs > kSumInPlace) sum_kernel<<<1, 1024, 0, s>>>(w.part, p->pairs, loss);
   return said(hipGetLastError());
 }
 
