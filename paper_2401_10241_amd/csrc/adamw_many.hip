@@ -73,52 +73,32 @@ template <bool NT, class V> __device__ __forceinline__ void put(void* p, V x) {
   if (NT) __builtin_nontemporal_store(x, (V*)p);
   else *(V*)p = x;
 }
-template <bool NT> __device__ __forceinline__ void load_f32(const float* p, int live, bool wide, float* x) {
-  if (wide) {
-    const f32x4 y = get<NT, f32x4>(p);
+template <class E> struct Vec;
+template <> struct Vec<float> { typedef f32x4 type; };
+template <> struct Vec<bf16_t> { typedef bf16x4 type; };
+template <bool NT, class E> __device__ __forceinline__ typename Vec<E>::type load4(const E* p, int live, bool wide) {
+  typedef typename Vec<E>::type V;
+  if (wide) return get<NT, V>(p);
+  V x;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = y[e];
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = e < live ? p[e] : 0.f;
-  }
+  for (int e = 0; e < 4; ++e) x[e] = e < live ? p[e] : (E)0.f;
+  return x;
 }
-template <bool NT> __device__ __forceinline__ void load_grad(const Tensor& q, long i, int live, bool wide, float* g) {
-  if (!(q.flags & kGrad16)) {
-    load_f32<NT>((const float*)q.grad + i, live, wide, g);
+template <bool NT, class E> __device__ __forceinline__ void store4(E* p, int live, bool wide, typename Vec<E>::type x) {
+  if (wide) {
+    put<NT>(p, x);
     return;
   }
-  const bf16_t* p = (const bf16_t*)q.grad + i;
-  if (wide) {
-    const bf16x4 x = get<NT, bf16x4>(p);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) g[e] = (float)x[e];
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) g[e] = e < live ? (float)p[e] : 0.f;
-  }
+  for (int e = 0; e < 4; ++e) if (e < live) p[e] = x[e];
 }
-template <bool NT> __device__ __forceinline__ void store_f32(float* p, int live, bool wide, const float* x) {
-  if (wide) {
-    f32x4 y;
+__device__ __forceinline__ f32x4 load_grad(const Tensor& q, long i, int live, bool wide) {
+  if (!(q.flags & kGrad16)) return load4<false, float>((const float*)q.grad + i, live, wide);
+  const bf16x4 x = load4<false, bf16_t>((const bf16_t*)q.grad + i, live, wide);
+  f32x4 y;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = x[e];
-    put<NT>(p, y);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) if (e < live) p[e] = x[e];
-  }
-}
-template <bool NT> __device__ __forceinline__ void store_bf16(bf16_t* p, int live, bool wide, const float* x) {
-  if (wide) {
-    bf16x4 y;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = (bf16_t)x[e];
-    put<NT>(p, y);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) if (e < live) p[e] = (bf16_t)x[e];
-  }
+  for (int e = 0; e < 4; ++e) y[e] = (float)x[e];
+  return y;
 }
 template <bool NT> __device__ __forceinline__ unsigned load_codes(const void* base, long i, int live, bool wide) {
   const unsigned char* p = (const unsigned char*)base + i;
@@ -172,38 +152,61 @@ struct Places {  // of four values one after the other
 };
 
 // Code of |m|: y = |m| / unit lies between c^2 and (c + 1)^2, and the upper code is taken if n / 131072 of the way is less than y - c^2
-// (n = 65536: the nearer one).  c comes from the root in 32 bits; where that is on the wrong side of a whole number, it is set right.
-__device__ __forceinline__ unsigned encode_m(double m, double inv, unsigned n) {
+// (n = 65536: the nearer one).  c comes from the root in 32 bits, which may be on the wrong side of a whole number by
+// 127 * 1.5 * 2^-23 at most: then y is that near to a code, and only an n within 3 of 0 or 131072 could take another one.  SURE sets c
+// right first, for those (risky()) and for values past the block's largest.
+template <bool SURE> __device__ __forceinline__ unsigned encode_m(double m, double inv, unsigned n) {
   const double y = fabs(m) * inv;
   int c = (int)__builtin_amdgcn_sqrtf((float)y);
-  c = c > 127 ? 127 : c;
-  double r = fma(-(double)c, (double)c, y);
-  int w = 2 * c + 1;
-  if (r < 0.0 || r >= (double)w) {
-    if (r < 0.0 && c > 0) --c;
-    else if (r >= (double)w && c < 127) ++c;
-    r = fma(-(double)c, (double)c, y);
-    w = 2 * c + 1;
+  if (SURE) {
+    c = c > 127 ? 127 : c;
+    if (c > 0 && (double)(c * c) > y) --c;
+    else if (c < 127 && (double)((c + 1) * (c + 1)) <= y) ++c;
   }
-  if (c < 127 && (double)((n & 0x3FFFFu) * ((unsigned)w & 0xFFu)) < r * 131072.0) ++c;
+  const double r = fma(-(double)c, (double)c, y);
+  const unsigned w = 2 * (unsigned)c + 1;
+  if ((double)((n & 0x3FFFFu) * (w & 0xFFu)) < r * 131072.0 && (!SURE || c < 127)) ++c;  // (at 127, r is too small unless SURE)
   return (unsigned)(m < 0 ? -c : c) & 0xFFu;
 }
-// The same for v between c^4 and (c + 1)^4; a positive v has code 1 at least.
-__device__ __forceinline__ unsigned encode_v(double x, double inv, unsigned n) {
+// The same for v between c^4 and (c + 1)^4, where the root of the root is off by 255 * 1.6 * 2^-23 at most and n within 6; a positive v has
+// code 1 at least.
+template <bool SURE> __device__ __forceinline__ unsigned encode_v(double x, double inv, unsigned n) {
   const double y = x * inv;
   int c = (int)__builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf((float)y));
-  c = c > 255 ? 255 : c;
-  double r = y - (double)fourth(c);
-  unsigned w = fourth(c + 1) - fourth(c);
-  if (r < 0.0 || r >= (double)w) {
-    if (r < 0.0 && c > 0) --c;
-    else if (r >= (double)w && c < 255) ++c;
-    r = y - (double)fourth(c);
-    w = fourth(c + 1) - fourth(c);
+  if (SURE) {
+    c = c > 255 ? 255 : c;
+    if (c > 0 && (double)fourth(c) > y) --c;
+    else if (c < 255 && (double)fourth(c + 1) <= y) ++c;
   }
-  if (c < 255 && (double)n * (double)w < r * 131072.0) ++c;
-  return c < 1 && y > 0.0 ? 1u : (unsigned)c;
+  const unsigned low = fourth(c);
+  const double r = y - (double)low;
+  if ((double)n * (double)(fourth(c + 1) - low) < r * 131072.0 && (!SURE || c < 255)) ++c;
+  return c < 1 && y > 0.0 ? 1u : (unsigned)c & 0xFFu;
 }
+// Remembers whether one of the numbers given is near the ends of its range: in halves of 16 bits, h < 4 or h >= 65532.
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+struct Ends {
+  u16x2 least = {0xFFFF, 0xFFFF};
+  __device__ __forceinline__ void see(unsigned h) {
+    union { unsigned u; u16x2 v; } x{h};
+    x.v += (u16x2){4, 4};
+    least = __builtin_elementwise_min(least, x.v);
+  }
+  __device__ __forceinline__ bool risky() const { return least[0] < 8 || least[1] < 8; }
+};
+template <bool SURE>
+__device__ __forceinline__ void encode_four(const double (&m)[4], const double (&v)[4], double im, double iv, const Places& at, Ends* ends, unsigned* wm,
+                                            unsigned* wv) {
+  *wm = *wv = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const unsigned h = at.number(e);
+    if (!SURE) ends->see(h);
+    *wm |= encode_m<SURE>(m[e], im, 2 * (h & 0xFFFFu) + 1) << (8 * e);
+    *wv |= encode_v<SURE>(v[e], iv, 2 * (h >> 16) + 1) << (8 * e);
+  }
+}
+
 // 1 / unit of a block whose largest value is `top`, from the hardware's reciprocal and two steps towards it; 0 gives every code 0
 __device__ __forceinline__ double inverse_of(float top, double unit) {
   const double u = (double)top * unit;
@@ -248,76 +251,122 @@ __device__ __forceinline__ float block_top(float v) {
   return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63));
 }
 
-// The step of four values of a lane from value i on; WHOLE: all lanes have them, aligned.  (Eight of an 8-bit state took 96 registers and
-// 1530 us where four take 1092, 315M values.)
-template <bool BITS8, bool WHOLE, bool NT>
-__device__ __forceinline__ void step_four(const Tensor& q, const Hyper& hp, const Clock& clk, long i) {
-  const int live = WHOLE ? 4 : live_of(q.n, i);
-  const bool wide = WHOLE || (live == 4 && (q.flags & kWide));
-  const float decay = q.flags & kDecay ? hp.decay : 0.f;
-  float g[4], th[4], m32[4], v32[4];
-  load_grad<NT>(q, i, live, wide, g);
-  load_f32<NT>(q.theta + i, live, wide, th);
-  if (!BITS8) {
-    load_f32<NT>((const float*)q.m + i, live, wide, m32);
-    load_f32<NT>((const float*)q.v + i, live, wide, v32);
+// The step of four values of a lane from value i on, in two parts so that the loads of the next four can be on their way before the
+// first are worked on; WHOLE: all lanes have four, aligned.
+template <bool BITS8, bool WHOLE, bool NT> struct Four {
+  long i;
+  int live;
+  bool wide, in;
+  f32x4 th, g, m, v;
+  bf16x4 g16;
+  unsigned cm, cv;
+  float tm, tv;
+
+  __device__ __forceinline__ void load(const Tensor& q, long at) {
+    i = at;
+    live = WHOLE ? 4 : live_of(q.n, i);
+    wide = WHOLE || (live == 4 && (q.flags & kWide));
+    if (q.flags & kGrad16) g16 = load4<NT, bf16_t>((const bf16_t*)q.grad + i, live, wide);
+    else g = load4<NT, float>((const float*)q.grad + i, live, wide);
+    th = load4<NT, float>(q.theta + i, live, wide);
+    if (BITS8) {
+      cm = load_codes<NT>(q.m, i, live, wide);
+      cv = load_codes<NT>(q.v, i, live, wide);
+      in = WHOLE || i / kBlock * kBlock < q.n;
+      tm = in ? q.m_scale[i / kBlock] : 0.f;
+      tv = in ? q.v_scale[i / kBlock] : 0.f;
+    } else {
+      m = load4<NT, float>((const float*)q.m + i, live, wide);
+      v = load4<NT, float>((const float*)q.v + i, live, wide);
+    }
+  }
+
+  __device__ __forceinline__ void move(const Tensor& q, const Hyper& hp, const Clock& clk) {
+    const float decay = q.flags & kDecay ? hp.decay : 0.f;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float ge = g[e] * clk.coef;
-      m32[e] = hp.b1f * m32[e] + hp.b1c * ge;
-      v32[e] = hp.b2f * v32[e] + hp.b2c * (ge * ge);
+      float x = th[e];
+      if (BITS8) move_theta_near(x, m[e], v[e], hp, decay, clk.ib1, clk.ib2);
+      else move_theta(x, m[e], v[e], hp, decay, clk.bc1, clk.bc2);
+      th[e] = x;
     }
-    store_f32<NT>((float*)q.m + i, live, wide, m32);
-    store_f32<NT>((float*)q.v + i, live, wide, v32);
-  } else {
-    const unsigned cm = load_codes<NT>(q.m, i, live, wide), cv = load_codes<NT>(q.v, i, live, wide);
-    const long block = i / kBlock;
-    const bool in = WHOLE || block * kBlock < q.n;
-    const double dm = in ? (double)q.m_scale[block] * (hp.b1 * kUnitM) : 0.0, dv = in ? (double)q.v_scale[block] * (hp.b2 * kUnitV) : 0.0;
-    double m[4], v[4];
-    float tm = 0.f, tv = 0.f;
+    store4<NT>(q.theta + i, live, wide, th);
+    if (q.copy16) {
+      bf16x4 c;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) c[e] = (bf16_t)th[e];
+      store4<NT>(q.copy16 + i, live, wide, c);
+    }
+  }
+
+  __device__ __forceinline__ void finish(const Tensor& q, const Hyper& hp, const Clock& clk) {
+    if (q.flags & kGrad16) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) g[e] = (float)g16[e];
+    }
+    if (!BITS8) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float ge = g[e] * clk.coef;
+        m[e] = hp.b1f * m[e] + hp.b1c * ge;
+        v[e] = hp.b2f * v[e] + hp.b2c * (ge * ge);
+      }
+      store4<NT>((float*)q.m + i, live, wide, m);
+      store4<NT>((float*)q.v + i, live, wide, v);
+      move(q, hp, clk);
+      return;
+    }
+    const double dm = (double)tm * (hp.b1 * kUnitM), dv = (double)tv * (hp.b2 * kUnitV);
+    double m64[4], v64[4];
+    float top_m = 0.f, top_v = 0.f;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const double ge = (double)g[e];
-      m[e] = value_m((int)(signed char)(cm >> (8 * e)), dm) + clk.km * ge;
-      v[e] = value_v((cv >> (8 * e)) & 0xFFu, dv) + clk.kv * (ge * ge);
-      m32[e] = (float)m[e];
-      v32[e] = (float)v[e];
-      tm = fmaxf(tm, fabsf(m32[e]));
-      tv = fmaxf(tv, v32[e]);
+      m64[e] = value_m((int)(signed char)(cm >> (8 * e)), dm) + clk.km * ge;
+      v64[e] = value_v((cv >> (8 * e)) & 0xFFu, dv) + clk.kv * (ge * ge);
+      m[e] = (float)m64[e];
+      v[e] = (float)v64[e];
+      top_m = fmaxf(top_m, fabsf(m[e]));
+      top_v = fmaxf(top_v, v[e]);
     }
-    tm = fminf(block_top(tm), kMostFloat);
-    tv = fminf(block_top(tv), kMostFloat);
-    const double im = inverse_of(tm, kUnitM), iv = inverse_of(tv, kUnitV);
+    move(q, hp, clk);  // (theta's registers are free then)
+    __builtin_amdgcn_sched_barrier(0);
+    top_m = fminf(block_top(top_m), kMostFloat);
+    top_v = fminf(block_top(top_v), kMostFloat);
+    const double im = inverse_of(top_m, kUnitM), iv = inverse_of(top_v, kUnitV);
     const Places at((unsigned long)(q.first + i), (unsigned long)clk.t, hp.seed);
-    unsigned wm = 0, wv = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const unsigned h = at.number(e);
-      wm |= encode_m(m[e], im, 2 * (h & 0xFFFFu) + 1) << (8 * e);
-      wv |= encode_v(v[e], iv, 2 * (h >> 16) + 1) << (8 * e);
-    }
+    unsigned wm, wv;
+    Ends ends;
+    encode_four<false>(m64, v64, im, iv, at, &ends, &wm, &wv);
+    if (ends.risky() || top_m >= kMostFloat || top_v >= kMostFloat) encode_four<true>(m64, v64, im, iv, at, &ends, &wm, &wv);
     store_codes<NT>(q.m, i, live, wide, wm);
     store_codes<NT>(q.v, i, live, wide, wv);
-    if (in && (threadIdx.x & 63) == 0) { q.m_scale[block] = tm; q.v_scale[block] = tv; }
+    if (in && (threadIdx.x & 63) == 0) { q.m_scale[i / kBlock] = top_m; q.v_scale[i / kBlock] = top_v; }
   }
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    if (BITS8) move_theta_near(th[e], m32[e], v32[e], hp, decay, clk.ib1, clk.ib2);
-    else move_theta(th[e], m32[e], v32[e], hp, decay, clk.bc1, clk.bc2);
-  }
-  store_f32<NT>(q.theta + i, live, wide, th);
-  if (q.copy16) store_bf16<NT>(q.copy16 + i, live, wide, th);
-}
+};
 
+constexpr int kRounds8 = 1, kRounds32 = 1;
 template <bool BITS8, bool NT>
 __global__ __launch_bounds__(kThreads) void adamw_many_kernel(Table tab, Hyper hp, const Clock* __restrict__ clk_at) {
+  constexpr int ROUNDS = BITS8 ? kRounds8 : kRounds32;
   const Clock clk = *clk_at;
   if (!clk.go) return;
   const Tensor& q = tensor_of(tab, blockIdx.x);
-  const long at = (long)(blockIdx.x - q.wg0) * kChunk, i = at + threadIdx.x * kPerThread;
-  if (q.n - at >= kChunk && (q.flags & kWide)) step_four<BITS8, true, NT>(q, hp, clk, i);
-  else step_four<BITS8, false, NT>(q, hp, clk, i);
+  const long at = (long)(blockIdx.x - q.wg0) * (kChunk * ROUNDS), i = at + threadIdx.x * kPerThread;
+  if (q.n - at >= kChunk * ROUNDS && (q.flags & kWide)) {
+    Four<BITS8, true, NT> f[ROUNDS];
+#pragma unroll
+    for (int k = 0; k < ROUNDS; ++k) f[k].load(q, i + k * kChunk);
+#pragma unroll
+    for (int k = 0; k < ROUNDS; ++k) f[k].finish(q, hp, clk);
+  } else {
+#pragma unroll 1
+    for (int k = 0; k < ROUNDS && at + k * kChunk < q.n; ++k) {
+      Four<BITS8, false, NT> f;
+      f.load(q, i + k * kChunk);
+      f.finish(q, hp, clk);
+    }
+  }
 }
 
 // moments held in 8 bits as values: Tensor.theta is where m's go, Tensor.grad v's
@@ -329,14 +378,14 @@ __global__ __launch_bounds__(kThreads) void read_moments_kernel(Table tab) {
   const bool wide = live == 4 && (q.flags & kWide);
   const unsigned cm = load_codes<false>(q.m, i, live, wide), cv = load_codes<false>(q.v, i, live, wide);
   const double um = (double)q.m_scale[i / kBlock] * kUnitM, uv = (double)q.v_scale[i / kBlock] * kUnitV;
-  float m[4], v[4];
+  f32x4 m, v;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     m[e] = (float)value_m((int)(signed char)(cm >> (8 * e)), um);
     v[e] = (float)value_v((cv >> (8 * e)) & 0xFFu, uv);
   }
-  store_f32<false>(q.theta + i, live, wide, m);
-  store_f32<false>((float*)q.grad + i, live, wide, v);
+  store4<false>(q.theta + i, live, wide, m);
+  store4<false>((float*)q.grad + i, live, wide, v);
 }
 
 // values into 8 bits, each to the nearer code
@@ -345,9 +394,8 @@ __global__ __launch_bounds__(kThreads) void write_moments_kernel(Table tab) {
   const long i = (long)(blockIdx.x - q.wg0) * kChunk + threadIdx.x * kPerThread;
   const int live = live_of(q.n, i);
   const bool wide = live == 4 && (q.flags & kWide);
-  float m[4], v[4], tm = 0.f, tv = 0.f;
-  load_f32<false>(q.theta + i, live, wide, m);
-  load_f32<false>((const float*)q.grad + i, live, wide, v);
+  float tm = 0.f, tv = 0.f;
+  const f32x4 m = load4<false, float>(q.theta + i, live, wide), v = load4<false, float>((const float*)q.grad + i, live, wide);
 #pragma unroll
   for (int e = 0; e < 4; ++e) { tm = fmaxf(tm, fabsf(m[e])); tv = fmaxf(tv, v[e]); }
   tm = fminf(block_top(tm), kMostFloat);
@@ -356,8 +404,8 @@ __global__ __launch_bounds__(kThreads) void write_moments_kernel(Table tab) {
   unsigned wm = 0, wv = 0;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    wm |= encode_m((double)m[e], im, 65536) << (8 * e);
-    wv |= encode_v((double)v[e], iv, 65536) << (8 * e);
+    wm |= encode_m<true>((double)m[e], im, 65536) << (8 * e);
+    wv |= encode_v<true>((double)v[e], iv, 65536) << (8 * e);
   }
   store_codes<false>(q.m, i, live, wide, wm);
   store_codes<false>(q.v, i, live, wide, wv);
@@ -378,8 +426,7 @@ __global__ __launch_bounds__(kThreads) void norm_many_kernel(Table tab, double* 
     const long i = i0 + (long)k * kChunk;
     const int live = live_of(q.n, i);
     if (!live) break;
-    float g[4];
-    load_grad<false>(q, i, live, live == 4 && (q.flags & kWide), g);
+    const f32x4 g = load_grad(q, i, live, live == 4 && (q.flags & kWide));
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       bad |= (__float_as_uint(g[e]) & 0x7F800000u) == 0x7F800000u ? 1 : 0;
@@ -536,7 +583,7 @@ zb_status zb_adamw_step(const zb_adamw_config* cfg, const zb_adamw_tensor* tenso
   for (int32_t k = 0; k < count; ++k) held += (double)tensors[k].n * (b8 ? 6 : 12);
   const bool nt = held > 256.0 * (1 << 20);
   const hipError_t e = for_tables(
-      tensors, count, kChunk,
+      tensors, count, kChunk * (b8 ? kRounds8 : kRounds32),
       [&](int32_t k, Tensor* q) {
         const zb_adamw_tensor& t = tensors[k];
         q->theta = t.theta; q->grad = t.grad; q->copy16 = (bf16_t*)t.copy16; q->m = t.m; q->v = t.v; q->m_scale = t.m_scale; q->v_scale = t.v_scale;
