@@ -43,6 +43,7 @@ static_assert(sizeof(Table) <= 3840, "launch arguments");
 
 struct Hyper {
   double b1, b2;
+  double log_b1, log_b2;
   float b1f, b1c, b2f, b2c, lr, eps, decay;  // b1c = 1 - b1
   double clip;
   unsigned seed;
@@ -216,23 +217,28 @@ __device__ __forceinline__ double inverse_of(float top, double unit) {
   return top > 0.f ? r : 0.0;
 }
 
-// whether to step, the clip coefficient, the time stamp and what depends on it
-__global__ void clock_kernel(Clock* k, Hyper hp, const double* sq, const int* nonfinite) {
-  k->go = 1;
+// Whether to step, the clip coefficient, the time stamp and what depends on it; two lanes, one for each average.
+__global__ __launch_bounds__(64) void clock_kernel(Clock* k, Hyper hp, const double* sq, const int* nonfinite) {
   double coef = 1.0;
   if (sq) {
-    k->go = !*nonfinite && isfinite(*sq) ? 1 : 0;
-    const double c = hp.clip / (sqrt(*sq) + 1e-6);
+    const double s = *sq;
+    if (*nonfinite || !isfinite(s)) {
+      if (threadIdx.x == 0) k->go = 0;
+      return;
+    }
+    const double c = hp.clip / (sqrt(s) + 1e-6);
     coef = c < 1.0 ? c : 1.0;
   }
-  if (!k->go) return;
-  k->t += 1;
-  const double bc1 = 1.0 - pow(hp.b1, (double)k->t), bc2 = 1.0 - pow(hp.b2, (double)k->t);
+  const long t = k->t + 1;
+  const bool second = threadIdx.x == 1;
+  const double bc = 1.0 - exp((double)t * (second ? hp.log_b2 : hp.log_b1));
+  if (threadIdx.x > 1) return;
+  (second ? k->bc2 : k->bc1) = (float)bc;
+  (second ? k->ib2 : k->ib1) = (float)(1.0 / bc);
+  if (second) return;
+  k->go = 1;
+  k->t = t;
   k->coef = (float)coef;
-  k->bc1 = (float)bc1;
-  k->bc2 = (float)bc2;
-  k->ib1 = (float)(1.0 / bc1);
-  k->ib2 = (float)(1.0 / bc2);
   k->km = coef * (1.0 - hp.b1);
   k->kv = coef * coef * (1.0 - hp.b2);
 }
@@ -414,50 +420,100 @@ __global__ __launch_bounds__(kThreads) void write_moments_kernel(Table tab) {
 }
 
 // ---- norm ---------------------------------------------------------------------------------------------------------
-constexpr int kNormChunk = 16 * kChunk;  // values of a workgroup
-__global__ __launch_bounds__(kThreads) void norm_many_kernel(Table tab, double* __restrict__ part_sq, int* __restrict__ part_nf) {
-  __shared__ double red[kThreads / 64];
-  __shared__ int redf[kThreads / 64];
-  const Tensor& q = tensor_of(tab, blockIdx.x);
-  const long i0 = (long)(blockIdx.x - q.wg0) * kNormChunk + threadIdx.x * kPerThread;
+constexpr int kNormVectors = 16, kNormChunk = kNormVectors * kChunk;  // values of a workgroup
+constexpr int kNormInPlace = 256;
+struct NormOut {
+  double* sq;
+  int* nf;
+  unsigned* done;  // null: a kernel of its own adds the parts
+};
+// Sum and flag of n parts by the THREADS lanes of a workgroup, in an order that only n decides; lane 0 writes them.
+template <int THREADS, class F> __device__ __forceinline__ void add_parts(long n, F&& part, double* sq, int* nf) {
+  __shared__ double red[THREADS / 64];
+  __shared__ int redf[THREADS / 64];
   double acc = 0.0;
   int bad = 0;
-  for (int k = 0; k < kNormChunk / kChunk; ++k) {
-    const long i = i0 + (long)k * kChunk;
-    const int live = live_of(q.n, i);
-    if (!live) break;
-    const f32x4 g = load_grad(q, i, live, live == 4 && (q.flags & kWide));
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      bad |= (__float_as_uint(g[e]) & 0x7F800000u) == 0x7F800000u ? 1 : 0;
-      acc += (double)g[e] * (double)g[e];
-    }
+  for (long i = threadIdx.x; i < n; i += THREADS) {
+    double x;
+    int f;
+    part(i, &x, &f);
+    acc += x;
+    bad |= f;
   }
   acc = wave_sum(acc);
   bad = __any(bad);
   if ((threadIdx.x & 63) == 0) { red[threadIdx.x >> 6] = acc; redf[threadIdx.x >> 6] = bad; }
   __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int w = 1; w < kThreads / 64; ++w) { acc += red[w]; bad |= redf[w]; }
-    part_sq[blockIdx.x] = acc;
-    part_nf[blockIdx.x] = bad;
-  }
+  if (threadIdx.x) return;
+  for (int w = 1; w < THREADS / 64; ++w) { acc += red[w]; bad |= redf[w]; }
+  *sq = acc;
+  *nf = bad ? 1 : 0;
 }
 __global__ __launch_bounds__(1024) void norm_sum_kernel(const double* __restrict__ part_sq, const int* __restrict__ part_nf, long parts,
                                                         double* __restrict__ sq_out, int* __restrict__ nf_out) {
-  __shared__ double red[1024];
-  __shared__ int redf[1024];
-  double acc = 0.0;
+  add_parts<1024>(parts, [&](long i, double* x, int* f) { *x = part_sq[i]; *f = part_nf[i]; }, sq_out, nf_out);
+}
+// One part per workgroup.  A launch of up to kNormInPlace of them adds the parts itself: the workgroup that is through last does, reading past
+// the caches of the XCDs what the others wrote past them; `done` counts modulo the workgroups, so it is 0 again for the next call.
+template <bool NT> __global__ __launch_bounds__(kThreads) void norm_many_kernel(Table tab, double* part_sq, int* part_nf, NormOut out) {
+  __shared__ double red[kThreads / 64];
+  __shared__ int redf[kThreads / 64];
+  __shared__ bool last;
+  const Tensor& q = tensor_of(tab, blockIdx.x);
+  const long start = (long)(blockIdx.x - q.wg0) * kNormChunk, i0 = start + threadIdx.x * kPerThread;
+  double acc[4] = {0.0, 0.0, 0.0, 0.0};
   int bad = 0;
-  for (long i = threadIdx.x; i < parts; i += 1024) { acc += part_sq[i]; bad |= part_nf[i]; }
-  red[threadIdx.x] = acc;
-  redf[threadIdx.x] = bad;
-  __syncthreads();
-  for (int o = 512; o > 0; o >>= 1) {
-    if ((int)threadIdx.x < o) { red[threadIdx.x] += red[threadIdx.x + o]; redf[threadIdx.x] |= redf[threadIdx.x + o]; }
-    __syncthreads();
+  auto take = [&](const f32x4& g) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      bad |= (__float_as_uint(g[e]) & 0x7F800000u) == 0x7F800000u ? 1 : 0;
+      acc[e] = fma((double)g[e], (double)g[e], acc[e]);
+    }
+  };
+  if (q.n - start >= kNormChunk && (q.flags & kWide)) {
+    if (q.flags & kGrad16) {  // eight loads on their way at a time
+      const bf16_t* p = (const bf16_t*)q.grad + start + threadIdx.x * 8;
+#pragma unroll
+      for (int k = 0; k < kNormVectors / 2; ++k) {
+        const bf16x8 x = get<NT, bf16x8>(p + (long)k * kThreads * 8);
+        const f32x4 a = {(float)x[0], (float)x[1], (float)x[2], (float)x[3]}, b = {(float)x[4], (float)x[5], (float)x[6], (float)x[7]};
+        take(a);
+        take(b);
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < kNormVectors; ++k) take(get<NT, f32x4>((const float*)q.grad + i0 + (long)k * kChunk));
+    }
+  } else {
+    for (int k = 0; k < kNormVectors; ++k) {
+      const long i = i0 + (long)k * kChunk;
+      const int live = live_of(q.n, i);
+      if (!live) break;
+      take(load_grad(q, i, live, live == 4 && (q.flags & kWide)));
+    }
   }
-  if (threadIdx.x == 0) { *sq_out = red[0]; *nf_out = redf[0] ? 1 : 0; }
+  double sum = wave_sum((acc[0] + acc[1]) + (acc[2] + acc[3]));
+  bad = __any(bad);
+  if ((threadIdx.x & 63) == 0) { red[threadIdx.x >> 6] = sum; redf[threadIdx.x >> 6] = bad; }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < kThreads / 64; ++w) { sum += red[w]; bad |= redf[w]; }
+    if (!out.done) {
+      part_sq[blockIdx.x] = sum;
+      part_nf[blockIdx.x] = bad;
+    } else {
+      __hip_atomic_store(part_sq + blockIdx.x, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __hip_atomic_store(part_nf + blockIdx.x, bad, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      last = __builtin_amdgcn_atomic_inc32(out.done, gridDim.x - 1, __ATOMIC_ACQ_REL, "agent") == gridDim.x - 1;
+    }
+  }
+  if (!out.done) return;
+  __syncthreads();
+  if (!last) return;
+  add_parts<kThreads>(gridDim.x, [&](long i, double* x, int* f) {
+    *x = __hip_atomic_load(part_sq + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    *f = __hip_atomic_load(part_nf + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }, out.sq, out.nf);
 }
 
 // ---- host ---------------------------------------------------------------------------------------------------------
@@ -505,12 +561,17 @@ hipError_t for_tables(const zb_adamw_tensor* t, int32_t count, long chunk, Fill&
   return tab.count ? start(tab, wgs) : hipSuccess;
 }
 
+int32_t live_tensors(const zb_adamw_tensor* t, int32_t count) {
+  int32_t n = 0;
+  for (int32_t k = 0; k < count; ++k) n += t[k].n > 0;
+  return n;
+}
 size_t norm_parts(const zb_adamw_tensor* t, int32_t count) {
   size_t n = 0;
   for (int32_t k = 0; k < count; ++k) n += (size_t)((t[k].n + kNormChunk - 1) / kNormChunk);
   return n;
 }
-bool wide_grad(const zb_adamw_tensor& t) { return !misaligned(t.grad, t.grad_dtype == ZB_BF16 ? 8 : 16); }
+bool wide_grad(const zb_adamw_tensor& t) { return !misaligned(t.grad, t.grad_dtype == ZB_BF16 ? 8 : 16); }  // for four values
 
 }  // namespace
 }  // namespace zb
@@ -536,18 +597,26 @@ zb_status zb_adamw_grad_norm(const zb_adamw_tensor* tensors, int32_t count, doub
   OnDeviceOf on(s);
   if (!on.ok) return ZB_EDEVICE;
   const size_t parts = norm_parts(tensors, count);
-  double* sq = (double*)workspace;
+  double* sq = (double*)((char*)workspace + 64);
   int* nf = (int*)(sq + parts);
+  const bool alone = parts > 0 && parts <= (size_t)kNormInPlace && live_tensors(tensors, count) <= kTensors;
+  const NormOut out{sq_out, nonfinite_out, alone ? (unsigned*)workspace : nullptr};
+  // gradients that no cache would hold until the step reads them again
+  double held = 0.0;
+  for (int32_t k = 0; k < count; ++k) held += (double)tensors[k].n * (tensors[k].grad_dtype == ZB_BF16 ? 2 : 4);
+  const bool nt = held > 256.0 * (1 << 20);
   size_t at = 0;
   hipError_t e = for_tables(
       tensors, count, kNormChunk,
-      [&](int32_t k, Tensor* q) { q->grad = tensors[k].grad; return wide_grad(tensors[k]); },
+      [&](int32_t k, Tensor* q) { q->grad = tensors[k].grad; return !misaligned(tensors[k].grad, 16); },
       [&](const Table& tab, unsigned wgs) {
-        norm_many_kernel<<<wgs, kThreads, 0, s>>>(tab, sq + at, nf + at);
+        if (nt) norm_many_kernel<true><<<wgs, kThreads, 0, s>>>(tab, sq + at, nf + at, out);
+        else norm_many_kernel<false><<<wgs, kThreads, 0, s>>>(tab, sq + at, nf + at, out);
         at += wgs;
         return hipGetLastError();
       });
   if (e != hipSuccess) return ZB_EDEVICE;
+  if (alone) return ZB_OK;
   norm_sum_kernel<<<1, 1024, 0, s>>>(sq, nf, (long)parts, sq_out, nonfinite_out);
   return hipGetLastError() == hipSuccess ? ZB_OK : ZB_EDEVICE;
 }
@@ -571,10 +640,10 @@ zb_status zb_adamw_step(const zb_adamw_config* cfg, const zb_adamw_tensor* tenso
   OnDeviceOf on(s);
   if (!on.ok) return ZB_EDEVICE;
   Hyper hp;
-  hp.b1 = cfg->beta1; hp.b2 = cfg->beta2;
+  hp.b1 = cfg->beta1; hp.b2 = cfg->beta2; hp.log_b1 = log(cfg->beta1); hp.log_b2 = log(cfg->beta2);
   hp.b1f = (float)cfg->beta1; hp.b1c = (float)(1.0 - cfg->beta1); hp.b2f = (float)cfg->beta2; hp.b2c = (float)(1.0 - cfg->beta2);
   hp.lr = (float)lr; hp.eps = (float)cfg->eps; hp.decay = (float)cfg->weight_decay; hp.clip = cfg->clip; hp.seed = cfg->seed;
-  clock_kernel<<<1, 1, 0, s>>>((Clock*)state, hp, sq, nonfinite);
+  clock_kernel<<<1, 64, 0, s>>>((Clock*)state, hp, sq, nonfinite);
   if (hipGetLastError() != hipSuccess) return ZB_EDEVICE;
   const bool b8 = cfg->bits == 8;
   // States that no cache would hold until the next step: more than the 256 MB of the last one.  us of 315M values with bf16 gradients with /
