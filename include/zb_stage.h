@@ -58,6 +58,8 @@ typedef enum { ZB_PASS_F = 0, ZB_PASS_B = 1, ZB_PASS_W = 2 } zb_pass;
 /* Sec. 5.1: the first stage of the pipeline also does the embedding lookup, the last one the loss
  * computation (each holds one transformer layer fewer to make up for it: pass that count as `layers`). */
 typedef enum { ZB_ROLE_MIDDLE = 0, ZB_ROLE_FIRST = 1, ZB_ROLE_LAST = 2 } zb_role;
+/* Loss of a last stage: softmax cross-entropy, or one of the losses on token log-probabilities further down. */
+typedef enum { ZB_LOSS_CROSS_ENTROPY = 0, ZB_LOSS_POLICY = 1, ZB_LOSS_PREFERENCE = 2 } zb_loss;
 typedef struct { int32_t pass, mb; } zb_op;
 
 /* Per-layer parameters, in the order used by every "param index" below. */
@@ -88,6 +90,13 @@ enum {
   ZB_T_TARGET_IDS = 69, /* last stage: target ids, same format                                         get/set */
   ZB_T_LOSS = 70,       /* last stage: mean over the tokens of microbatch mb of its cross-entropy loss
                            (written by F), one fp32                                                    get */
+  /* last stage with a policy or preference loss: fp32 [tokens] of microbatch mb unless said otherwise, zero until set */
+  ZB_T_LOSS_WEIGHT = 71, /* weight of each token; 0: it does not count                                   get/set */
+  ZB_T_ADVANTAGE = 72,   /* policy                                                                      get/set */
+  ZB_T_OLD_LOGP = 73,    /* policy: log-probabilities of the targets when they were drawn                get/set */
+  ZB_T_REF_LOGP = 74,    /* log-probabilities of the targets under the reference                        get/set */
+  ZB_T_TOKEN_LOGP = 75,  /* log-probabilities of the targets of weight (written by F), 0 for the others  get */
+  ZB_T_REWARDS = 76,     /* preference: [mb_size], pref_beta * sum of weight * (logp - ref) of each sample (written by F)  get */
   ZB_T_STAGE_PARAM = 96,    /* + ZB_SP_*: stage-level master parameter (layer, mb ignored)              get/set */
   ZB_T_STAGE_GRAD = 104,    /* + ZB_SP_*: its accumulated gradient                                      get/set */
   ZB_T_STAGE_ADAM_M = 112,  /* + ZB_SP_*                                                                get/set */
@@ -131,10 +140,18 @@ typedef struct {
   void* hip_stream;         /* hipStream_t or NULL */
   void* arena;              /* device memory, 256-byte aligned */
   size_t arena_bytes;
+  int32_t loss;             /* zb_loss of a last stage.  With ZB_LOSS_POLICY, LOSS of a microbatch is zb_policy_loss's with scale
+                               1 / tokens; with ZB_LOSS_PREFERENCE, zb_preference_loss's with scale 1 / pairs, samples 2i (preferred)
+                               and 2i + 1 being a pair (mb_size even).  B starts from the gradient of the mean of LOSS over the
+                               iteration's m microbatches; F computes it in the place of the logits and keeps it for B and W, so the
+                               tensors above must be set before F */
+  double clip_low, clip_high, kl_coef; /* policy */
+  double pref_beta, label_smoothing;   /* preference */
 } zb_config;
 
 /* Fills the numeric fields of *cfg with defaults (ln_eps 1e-5, lr 1e-4, betas 0.9/0.95,
- * eps 1e-8, weight decay 0.01, clip 1.0, journal 1, group_w 1, dtype bf16); shapes are left 0. */
+ * eps 1e-8, weight decay 0.01, clip 1.0, journal 1, group_w 1, dtype bf16, clip_low and clip_high 0.2, pref_beta 0.1);
+ * shapes are left 0. */
 zb_status zb_config_defaults(zb_config* cfg);
 
 /* Device bytes zb_stage_init needs for this configuration (arena fields ignored). */

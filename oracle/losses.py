@@ -9,8 +9,13 @@ lies in [0, vocab) and its weight is not zero; the others have logp 0 and no gra
    loss = scale * sum_i -(1 - eps) log sigma(x) - eps log sigma(-x).
 
 Both gradients are written out by the chain rule through c_r = d loss / d logp_r:
-d loss / d z_rj = c_r ([j = t(r)] - exp(z_rj - lse_r)).  tests/test_oracle_losses.py pins them to differences."""
+d loss / d z_rj = c_r ([j = t(r)] - exp(z_rj - lse_r)).  tests/test_oracle_losses.py pins them to differences.  `LossStageOracle`
+puts them behind a last stage's layers."""
 import numpy as np
+
+from .endstages import EndStageOracle
+from .layers import layernorm_bwd_input, layernorm_fwd
+from .stage import StageOracle
 
 
 def counting(targets, vocab, weight=None, offsets=None):
@@ -80,3 +85,42 @@ def preference(z, targets, ref, offsets, weight=None, beta=0.1, eps=0.0, scale=1
         for q, sign in ((2 * i, 1), (2 * i + 1, -1)):
             c[offsets[q]:offsets[q + 1]] = sign * slope * w[offsets[q]:offsets[q + 1]]
     return loss, logp, beta * sums, c, dlogits(z, targets, lse, c, on)
+
+
+class LossStageOracle(EndStageOracle):
+    """Last stage with one of the two losses: LOSS of a microbatch is the mean over its tokens (policy) or pairs (preference,
+    samples 2i and 2i + 1, the preferred one first); B starts from the gradient of the mean over the m microbatches."""
+
+    def __init__(self, *, kind, low=0.2, high=0.2, kl=0.0, beta=0.1, eps=0.0, **kw):
+        assert kind in ("policy", "preference")
+        self.kind, self.low, self.high, self.kl, self.beta, self.eps = kind, low, high, kl, beta, eps
+        super().__init__(role="last", **kw)
+
+    def begin_iteration(self, m):
+        super().begin_iteration(m)
+        self.values, self.logp, self.rewards = {}, {}, {}
+
+    def set_values(self, mb, **values):
+        """weight, ref and, for a policy, old and advantage."""
+        self.values[mb] = values
+
+    def forward(self, mb):
+        StageOracle.forward(self, mb)
+        ex, v, t = self.work_extra, self.values[mb], self.targets[mb]
+        Z, xhat, r = layernorm_fwd(np.asarray(self.Y[mb], np.float64), ex["lnf_g"], ex["lnf_b"], self.ln_eps)
+        z = Z @ ex["w_head"]
+        if self.kind == "policy":
+            self.loss[mb], self.logp[mb], _, d = policy(z, t, v["old"], v["advantage"], v["ref"], v["weight"], self.low, self.high, self.kl, 1.0 / t.size)
+        else:
+            off = np.arange(self.b + 1) * self.s
+            self.loss[mb], self.logp[mb], self.rewards[mb], _, d = preference(z, t, v["ref"], off, v["weight"], self.beta, self.eps, 2.0 / self.b)
+        self._head[mb] = (d / self.m, Z, xhat, r)
+
+    def backward_input(self, mb):
+        ex = self.work_extra
+        d, Z, xhat, r = self._head.pop(mb)
+        self._head_w[mb] = dict(Z=Z, dlogits=d)
+        self.dY[mb], dg, db = layernorm_bwd_input(d @ ex["w_head"].T, xhat, r, ex["lnf_g"])
+        self.grads[self.nl]["lnf_g"] += dg
+        self.grads[self.nl]["lnf_b"] += db
+        StageOracle.backward_input(self, mb)

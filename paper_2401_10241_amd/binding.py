@@ -37,6 +37,8 @@ T_INPUT_X, T_INPUT_DY, T_OUTPUT_Y, T_OUTPUT_DX = 64, 65, 66, 67
 T_FLAT_PARAMS, T_FLAT_GRADS, T_FLAT_ADAM_M, T_FLAT_ADAM_V = 80, 81, 82, 83
 T_INPUT_IDS, T_TARGET_IDS, T_LOSS = 68, 69, 70
 T_STAGE_PARAM, T_STAGE_GRAD, T_STAGE_ADAM_M, T_STAGE_ADAM_V = 96, 104, 112, 120
+T_LOSS_WEIGHT, T_ADVANTAGE, T_OLD_LOGP, T_REF_LOGP, T_TOKEN_LOGP, T_REWARDS = range(71, 77)
+LOSS = {"cross_entropy": 0, "policy": 1, "preference": 2}
 ROLE = {"middle": 0, "first": 1, "last": 2}
 STAGE_PARAM_INDEX = {"emb_tok": 0, "emb_pos": 1, "lnf_g": 2, "lnf_b": 3, "w_head": 4}
 S_QKV_IN, S_PROJ_IN, S_FC1_IN, S_FC2_IN, S_QKV_DOUT, S_PROJ_DOUT, S_FC1_DOUT, S_FC2_DOUT = range(8)
@@ -56,7 +58,9 @@ class zb_config(C.Structure):
                 ("ln_eps", C.c_float), ("lr", C.c_float),
                 ("beta1", C.c_float), ("beta2", C.c_float), ("adam_eps", C.c_float),
                 ("weight_decay", C.c_float), ("clip", C.c_float), ("hip_stream", C.c_void_p),
-                ("arena", C.c_void_p), ("arena_bytes", C.c_size_t)]
+                ("arena", C.c_void_p), ("arena_bytes", C.c_size_t),
+                ("loss", C.c_int32), ("clip_low", C.c_double), ("clip_high", C.c_double), ("kl_coef", C.c_double),
+                ("pref_beta", C.c_double), ("label_smoothing", C.c_double)]
 
 
 class zb_global_state(C.Structure):
@@ -489,7 +493,8 @@ class Stage:
     def __init__(self, *, layers, hidden, heads, ffn, seq, mb_size=1, dtype="bf16", max_microbatches,
                  max_pending_b, max_pending_w, max_inflight, journal=True, group_w=True, fuse_bw=False, chunks=1,
                  role="middle", vocab=0, ln_eps=1e-5, lr=1e-4, beta1=0.9,
-                 beta2=0.95, adam_eps=1e-8, weight_decay=0.01, clip=1.0, device="cuda:0", stream=None):
+                 beta2=0.95, adam_eps=1e-8, weight_decay=0.01, clip=1.0, device="cuda:0", stream=None, loss="cross_entropy",
+                 clip_low=0.2, clip_high=0.2, kl_coef=0.0, pref_beta=0.1, label_smoothing=0.0):
         import torch
         if not torch.cuda.is_available():
             raise RuntimeError("no GPU: the zero-bubble stage runs only on the device (no CPU fallback)")
@@ -509,6 +514,9 @@ class Stage:
         self.role, self.vocab, self.seq = role, vocab, seq
         cfg.ln_eps, cfg.lr, cfg.beta1, cfg.beta2 = ln_eps, lr, beta1, beta2
         cfg.adam_eps, cfg.weight_decay, cfg.clip = adam_eps, weight_decay, clip
+        cfg.loss = LOSS[loss]
+        cfg.clip_low, cfg.clip_high, cfg.kl_coef = clip_low, clip_high, kl_coef
+        cfg.pref_beta, cfg.label_smoothing = pref_beta, label_smoothing
         need = C.c_size_t(0)
         rc = lib.zb_stage_arena_bytes(C.byref(cfg), C.byref(need))
         if rc != OK:
@@ -599,6 +607,17 @@ class Stage:
 
     def get_ids(self, what: int, mb: int) -> np.ndarray:
         out = np.empty(self.tokens, np.int32)
+        self._call(lib.zb_get_tensor, what, 0, mb, out.ctypes.data_as(C.c_void_p), out.nbytes)
+        return out
+
+    def set_token_values(self, what: int, mb: int, values):
+        """zb_set_tensor for T_LOSS_WEIGHT / T_ADVANTAGE / T_OLD_LOGP / T_REF_LOGP: fp32 [tokens]."""
+        v = np.ascontiguousarray(values, np.float32)
+        self._call(lib.zb_set_tensor, what, 0, mb, v.ctypes.data_as(C.c_void_p), v.nbytes)
+
+    def get_token_values(self, what: int, mb: int) -> np.ndarray:
+        """zb_get_tensor for the same, T_TOKEN_LOGP ([tokens]) and T_REWARDS ([mb_size])."""
+        out = np.empty(self.cfg.mb_size if what == T_REWARDS else self.tokens, np.float32)
         self._call(lib.zb_get_tensor, what, 0, mb, out.ctypes.data_as(C.c_void_p), out.nbytes)
         return out
 

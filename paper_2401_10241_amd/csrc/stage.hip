@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "../../include/zb_stage.h"
+#include "token_loss.h"
 #include "zb_common.h"
 
 using namespace zb;
@@ -40,12 +41,12 @@ struct LayerOff {  // byte offsets inside one slot of each pool
 
 enum KClass {
   KC_GEMM_FWD = 0, KC_GEMM_DGRAD, KC_GEMM_WGRAD, KC_ATTN_FWD, KC_ATTN_BWD, KC_LN_FWD, KC_LN_BWD,
-  KC_FILL, KC_SUMSQ, KC_ADAMW_STEP, KC_ADAMW_ROLLBACK, KC_ADAMW_RESTEP, KC_TRANSPOSE, KC_EMBED, KC_LOSS, KC_COUNT
+  KC_FILL, KC_SUMSQ, KC_ADAMW_STEP, KC_ADAMW_ROLLBACK, KC_ADAMW_RESTEP, KC_TRANSPOSE, KC_EMBED, KC_LOSS, KC_TOKEN_LOSS, KC_COUNT
 };
 const char* const kClassNames[KC_COUNT] = {
     "gemm_fwd", "gemm_dgrad", "gemm_wgrad", "attention_fwd", "attention_bwd", "layernorm_fwd", "layernorm_bwd",
     "grad_zero_fill", "grad_sumsq", "adamw_step", "adamw_rollback", "adamw_restep",
-    "weight_transpose", "embedding", "cross_entropy"};
+    "weight_transpose", "embedding", "cross_entropy", "token_loss"};
 
 struct ProfRec {
   int cls;
@@ -89,6 +90,12 @@ struct zb_stage {
   int *ids = nullptr, *perm = nullptr;  // [max_microbatches][T]: input ids (first) / target ids (last); sorted token order
   float *loss = nullptr, *row_loss = nullptr;
   size_t fb_logits = 0, fb_lse = 0, fb_statsf = 0, fw_z = 0, bw_dlogits = 0;  // last stage: offsets inside the stash slots
+  // policy and preference loss: F leaves the gradient where it found the logits, F -> W; per microbatch [T] what the loss reads, and logp
+  size_t fw_logits = 0;
+  float *tok_weight = nullptr, *tok_adv = nullptr, *tok_old = nullptr, *tok_ref = nullptr, *tok_logp = nullptr, *rewards = nullptr;
+  int* offsets = nullptr;  // of a microbatch's samples
+  char* loss_ws = nullptr;
+  size_t loss_ws_bytes = 0;
   float* SP(int i) const { return theta + spoff[i]; }
   float* SG(int i) const { return grad + spoff[i]; }
   const void* SWt(int i) const { return bf16 ? (const void*)(theta16 + spoff[i]) : (const void*)SP(i); }
@@ -172,9 +179,25 @@ bool valid_shapes(const zb_config* c, std::string* why) {
   if (c->chunks != 0 && c->chunks != 1 && c->chunks != 2) return bad("chunks must be 1 or 2");
   if (c->chunks == 2 && c->layers % 2 != 0) return bad("two chunks need an even number of layers");
   if (c->role != ZB_ROLE_MIDDLE && c->role != ZB_ROLE_FIRST && c->role != ZB_ROLE_LAST) return bad("unknown role");
+  if (c->role == ZB_ROLE_MIDDLE && c->loss != ZB_LOSS_CROSS_ENTROPY) return bad("only a last stage has a loss");
   if (c->role != ZB_ROLE_MIDDLE) {
     if (c->chunks == 2) return bad("a first or last stage cannot hold two chunks");
     if (c->vocab < 1 || c->vocab > kEmbeddingMaxVocab) return bad("vocab must be in [1, 2^18]");
+    if (c->loss != ZB_LOSS_CROSS_ENTROPY) {
+      if (c->role != ZB_ROLE_LAST) return bad("only a last stage has a loss");
+      if (c->loss == ZB_LOSS_POLICY) {
+        zb_policy p{};
+        p.clip_low = c->clip_low; p.clip_high = c->clip_high; p.kl_coef = c->kl_coef; p.scale = 1.0;
+        if (!valid_policy(&p)) return bad("clip_low must be in [0, 1], clip_high and kl_coef finite and not negative");
+      } else if (c->loss == ZB_LOSS_PREFERENCE) {
+        zb_preference p{};
+        p.beta = c->pref_beta; p.label_smoothing = c->label_smoothing; p.scale = 1.0;
+        if (!valid_preference(&p)) return bad("pref_beta must be finite, label_smoothing in [0, 1]");
+        if (c->mb_size % 2 != 0) return bad("the samples of a microbatch are pairs: mb_size must be even");
+      } else {
+        return bad("unknown loss");
+      }
+    }
     if (c->role == ZB_ROLE_FIRST && (long long)c->seq * c->mb_size > kEmbeddingMaxTokens)
       return bad("a first stage takes at most 8192 tokens per microbatch");
   }
@@ -261,11 +284,15 @@ size_t layout(zb_stage* st, void* arena) {
     q.bw_dy = put(obw, l == st->L - 1 ? 0 : T * h * E);
   }
   if (c.role == ZB_ROLE_LAST) {  // the head: logits and row statistics F -> B, its input F -> W, its output gradient B -> W
-    st->fb_logits = put(ofb, T * (size_t)st->V * E);
-    st->fb_lse = put(ofb, T * sizeof(float));
+    if (c.loss == ZB_LOSS_CROSS_ENTROPY) {
+      st->fb_logits = put(ofb, T * (size_t)st->V * E);
+      st->fb_lse = put(ofb, T * sizeof(float));
+      st->bw_dlogits = put(obw, T * (size_t)st->V * E);
+    } else {
+      st->fw_logits = put(ofw, T * (size_t)st->V * E);
+    }
     st->fb_statsf = put(ofb, T * 2 * sizeof(float));
     st->fw_z = put(ofw, T * h * E);
-    st->bw_dlogits = put(obw, T * (size_t)st->V * E);
   }
   st->fb_slot = ofb; st->fw_slot = ofw; st->bw_slot = obw;
   st->fb_pool = bp.take<char>(ofb * (size_t)c.max_pending_b);
@@ -277,6 +304,21 @@ size_t layout(zb_stage* st, void* arena) {
   if (c.role == ZB_ROLE_LAST) {
     st->loss = bp.take<float>((size_t)c.max_microbatches * sizeof(float));
     st->row_loss = bp.take<float>(T * sizeof(float));
+    if (c.loss != ZB_LOSS_CROSS_ENTROPY) {
+      const size_t each = (size_t)c.max_microbatches * T * sizeof(float);
+      st->tok_weight = bp.take<float>(each);
+      st->tok_ref = bp.take<float>(each);
+      st->tok_logp = bp.take<float>(each);
+      if (c.loss == ZB_LOSS_POLICY) {
+        st->tok_adv = bp.take<float>(each);
+        st->tok_old = bp.take<float>(each);
+      } else {
+        st->rewards = bp.take<float>((size_t)c.max_microbatches * c.mb_size * sizeof(float));
+        st->offsets = bp.take<int>(((size_t)c.mb_size + 1) * sizeof(int));
+      }
+      st->loss_ws_bytes = loss_workspace_bytes((int)T, c.mb_size / 2);
+      st->loss_ws = bp.take<char>(st->loss_ws_bytes);
+    }
   }
   st->tmp = bp.take<char>(T * h * E);
   st->dvec = bp.take<float>((size_t)st->b * st->a * st->s * sizeof(float));
@@ -459,7 +501,7 @@ template <typename T> struct Exec {
     }
     if (st->role == ZB_ROLE_LAST) {  // final LayerNorm, head, softmax cross-entropy against the targets
       T* Z = (T*)(fw + st->fw_z);
-      T* logits = (T*)(fb + st->fb_logits);
+      T* logits = (T*)(st->cfg.loss == ZB_LOSS_CROSS_ENTROPY ? fb + st->fb_logits : fw + st->fw_logits);
       {
         ProfScope ps(st, KC_LN_FWD, 0, 2 * E * T_ * h + 8.0 * T_);
         ZB_HIP(st, launch_layernorm_fwd<T>(x, st->SP(ZB_SP_LNF_G), st->SP(ZB_SP_LNF_B), Z, (float*)(fb + st->fb_statsf),
@@ -470,6 +512,7 @@ template <typename T> struct Exec {
       g.a_sm = h; g.a_sk = 1; g.b_sk = st->V; g.b_sn = 1;
       g.epilogue = EPI_STORE; g.out0 = logits;
       ZB_HIP(st, gemm(st, KC_GEMM_FWD, g));
+      if (st->cfg.loss != ZB_LOSS_CROSS_ENTROPY) return token_loss(st, mb, logits);
       ProfScope ps(st, KC_LOSS, 0, E * T_ * (double)st->V);
       ZB_HIP(st, launch_ce_fwd<T>(logits, st->ids + (size_t)mb * T_, (float*)(fb + st->fb_lse), st->row_loss,
                                   st->loss + mb, T_, st->V, s));
@@ -477,16 +520,46 @@ template <typename T> struct Exec {
     return ZB_OK;
   }
 
-  // Last stage: the gradient that starts B.  dLogits = (softmax - onehot) / (tokens * m) is kept for W, goes
+  // Policy or preference loss of a microbatch, and in the place of its logits their gradient: the mean over the iteration's
+  // microbatches of their means over tokens or pairs.
+  static zb_status token_loss(zb_stage* st, int mb, T* logits) {
+    const zb_config& c = st->cfg;
+    const size_t at = (size_t)mb * st->T;
+    zb_logits x{};
+    x.logits = logits; x.targets = st->ids + at; x.row_stride = st->V; x.rows = st->T; x.vocab = st->V; x.dtype = c.dtype;
+    const double bytes = sizeof(T) * (double)st->T * st->V;
+    ProfScope ps(st, KC_TOKEN_LOSS, 0, (c.loss == ZB_LOSS_POLICY ? 2 : 3) * bytes);
+    zb_status rc;
+    if (c.loss == ZB_LOSS_POLICY) {
+      zb_policy p{};
+      p.old_logp = st->tok_old + at; p.advantage = st->tok_adv + at; p.ref_logp = st->tok_ref + at; p.weight = st->tok_weight + at;
+      p.clip_low = c.clip_low; p.clip_high = c.clip_high; p.kl_coef = c.kl_coef; p.scale = 1.0 / st->T;
+      rc = policy_loss(&x, &p, p.scale / st->m, st->loss + mb, st->tok_logp + at, logits, 0, st->loss_ws, st->loss_ws_bytes, st->stream);
+    } else {
+      zb_preference p{};
+      p.ref_logp = st->tok_ref + at; p.weight = st->tok_weight + at; p.offsets = st->offsets; p.pairs = c.mb_size / 2;
+      p.beta = c.pref_beta; p.label_smoothing = c.label_smoothing; p.scale = 1.0 / p.pairs;
+      rc = preference_loss(&x, &p, p.scale / st->m, st->loss + mb, st->tok_logp + at, st->rewards + (size_t)mb * c.mb_size, logits, 0, st->loss_ws,
+                           st->loss_ws_bytes, st->stream);
+    }
+    return rc == ZB_OK ? ZB_OK : fail(st, rc, "token loss");
+  }
+
+  // Where the gradient of the logits is kept between F or B and W.
+  static T* dlogits_of(zb_stage* st, int mb) {
+    if (st->cfg.loss == ZB_LOSS_CROSS_ENTROPY) return (T*)(st->bw_pool + st->bw_slot * (size_t)st->slot_bw[mb] + st->bw_dlogits);
+    return (T*)(st->fw_pool + st->fw_slot * (size_t)st->slot_fw[mb] + st->fw_logits);
+  }
+
+  // Last stage: the gradient that starts B.  Cross-entropy's dLogits = (softmax - onehot) / (tokens * m) is kept for W, goes
   // through the head and the final LayerNorm, and lands where a middle stage receives the upstream gradient.
   static zb_status head_backward(zb_stage* st, int mb) {
     const int h = st->h, T_ = st->T;
     hipStream_t s = st->stream;
     char* fb = st->fb_pool + st->fb_slot * (size_t)st->slot_fb[mb];
-    char* bw = st->bw_pool + st->bw_slot * (size_t)st->slot_bw[mb];
     const double E = sizeof(T);
-    T* dlogits = (T*)(bw + st->bw_dlogits);
-    {
+    T* dlogits = dlogits_of(st, mb);
+    if (st->cfg.loss == ZB_LOSS_CROSS_ENTROPY) {  // (the other losses leave theirs in F)
       ProfScope ps(st, KC_LOSS, 0, 2 * E * T_ * (double)st->V);
       ZB_HIP(st, launch_ce_bwd<T>((const T*)(fb + st->fb_logits), (const float*)(fb + st->fb_lse),
                                   st->ids + (size_t)mb * T_, dlogits, T_, st->V, 1.0f / ((float)T_ * (float)st->m), s));
@@ -518,7 +591,7 @@ template <typename T> struct Exec {
       w.M[0] = h; w.N[0] = st->V; w.outf[0] = st->SG(ZB_SP_W_HEAD);
       for (int i = 0; i < n; ++i) {
         w.a[i] = st->fw_pool + st->fw_slot * (size_t)st->slot_fw[mbs[i]] + st->fw_z;
-        w.b[i] = st->bw_pool + st->bw_slot * (size_t)st->slot_bw[mbs[i]] + st->bw_dlogits;
+        w.b[i] = dlogits_of(st, mbs[i]);
       }
       ProfScope ps(st, KC_GEMM_WGRAD, 2.0 * h * st->V * T_ * n, 8.0 * h * st->V + E * (double)T_ * ((double)h + st->V) * n);
       ZB_HIP(st, launch_wgrad_multi<T>(w, s));
@@ -786,6 +859,16 @@ zb_status resolve(zb_stage* st, int what, int layer, int mb, TensorRef* r) {
     r->writable = false;
     return ZB_OK;
   }
+  if (what >= ZB_T_LOSS_WEIGHT && what <= ZB_T_REWARDS) {
+    float* base = what == ZB_T_LOSS_WEIGHT ? st->tok_weight : what == ZB_T_ADVANTAGE ? st->tok_adv : what == ZB_T_OLD_LOGP ? st->tok_old
+                : what == ZB_T_REF_LOGP ? st->tok_ref : what == ZB_T_TOKEN_LOGP ? st->tok_logp : st->rewards;
+    if (!base) return fail(st, ZB_EINVAL, "the stage's loss has no such tensor");
+    if (mb < 0 || mb >= st->cfg.max_microbatches) return fail(st, ZB_EINVAL, "microbatch out of range");
+    r->count = what == ZB_T_REWARDS ? (size_t)st->b : (size_t)st->T;
+    r->ptr = base + (size_t)mb * r->count;
+    r->writable = what < ZB_T_TOKEN_LOGP;
+    return ZB_OK;
+  }
   if (what >= ZB_T_STAGE_PARAM && what < ZB_T_STAGE_ADAM_V + 8) {
     const int grp = (what - ZB_T_STAGE_PARAM) / 8, i = (what - ZB_T_STAGE_PARAM) % 8;
     if (i >= ZB_SP_COUNT || st->spcount[i] == 0) return fail(st, ZB_EINVAL, "this stage has no such stage-level parameter");
@@ -824,6 +907,8 @@ zb_status zb_config_defaults(zb_config* cfg) {
   cfg->ln_eps = 1e-5f;
   cfg->lr = 1e-4f; cfg->beta1 = 0.9f; cfg->beta2 = 0.95f; cfg->adam_eps = 1e-8f; cfg->weight_decay = 0.01f;
   cfg->clip = 1.0f;
+  cfg->clip_low = cfg->clip_high = 0.2;
+  cfg->pref_beta = 0.1;
   return ZB_OK;
 }
 
@@ -856,6 +941,11 @@ zb_status zb_stage_init(const zb_config* cfg, zb_stage** out) {
   for (int i = 0; i < KC_COUNT; ++i) st->prof_flops[i] = st->prof_bytes[i] = 0;
   // zero state: parameters, moments, gradients, journal, optimizer scalars
   hipError_t e = hipMemsetAsync(cfg->arena, 0, need, st->stream);
+  std::vector<int> offsets;
+  if (e == hipSuccess && st->offsets) {
+    for (int q = 0; q <= cfg->mb_size; ++q) offsets.push_back(q * cfg->seq);
+    e = hipMemcpyAsync(st->offsets, offsets.data(), offsets.size() * sizeof(int), hipMemcpyHostToDevice, st->stream);
+  }
   if (e == hipSuccess) e = hipStreamSynchronize(st->stream);
   if (e != hipSuccess) {
     delete st;

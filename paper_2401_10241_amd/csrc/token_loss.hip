@@ -5,8 +5,7 @@
 // the logits of the others are not read.
 #include <math.h>
 
-#include "../../include/zb_stage.h"
-#include "zb_common.h"
+#include "token_loss.h"
 
 namespace zb {
 
@@ -130,7 +129,7 @@ template <typename T, bool NT> __device__ __forceinline__ void clear_row(T* d, i
 
 struct PolicyArgs {
   const float *old_logp, *ref_logp, *advantage;
-  double lo, hi, log_lo, log_hi, kl, scale;  // borders of the ratio and of its logarithm
+  double lo, hi, log_lo, log_hi, kl, scale, grad_scale;  // borders of the ratio and of its logarithm
 };
 // exp(d) to the last bit or two of fp32, whatever the size of d
 __device__ __forceinline__ double exp_near(double d) {
@@ -151,7 +150,7 @@ __device__ __forceinline__ double exp_above_line(double d) {
 // Loss of a row and its derivative by the row's log-probability.  One lane does this while the others wait, so it takes the
 // exponential of fp32; what is compared with a border is the logarithm, in 64 bits.
 __device__ __forceinline__ double policy_row(const PolicyArgs& a, const Rows& of, int row, double logp, double* slope) {
-  const double adv = a.advantage[row], x = logp - (double)a.old_logp[row], rho = exp_near(x), w = of.weight_of(row) * a.scale;
+  const double adv = a.advantage[row], x = logp - (double)a.old_logp[row], rho = exp_near(x), w = of.weight_of(row);
   const bool above = x > a.log_hi, below = x < a.log_lo;
   const double held = above ? a.hi : below ? a.lo : rho;
   double loss = -fmin(rho * adv, held * adv);
@@ -161,8 +160,8 @@ __device__ __forceinline__ double policy_row(const PolicyArgs& a, const Rows& of
     loss += a.kl * k;
     g -= a.kl * (k + d);
   }
-  *slope = w * g;
-  return w * loss;
+  *slope = a.grad_scale * w * g;
+  return a.scale * w * loss;
 }
 
 // Sum of n values by the THREADS lanes of a workgroup, in an order that only n decides; lane 0 has it.
@@ -476,7 +475,7 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(const T* logits, long st
 
 struct PairArgs {
   const float* ref_logp;
-  double beta, smoothing, scale;
+  double beta, smoothing, scale, grad_scale;
 };
 __device__ __forceinline__ void sequence_rows(const int* offsets, int q, int rows, int* a, int* b) {
   const int x = offsets[q], y = offsets[q + 1];
@@ -510,7 +509,7 @@ __global__ __launch_bounds__(kThreads) void pair_kernel(PairArgs a, Rows of, int
     loss = a.scale * ((1.0 - a.smoothing) * (fmax(-x, 0.0) + l) + a.smoothing * (fmax(x, 0.0) + l));
     const double above = x >= 0 ? 1.0 / (1.0 + e) : e / (1.0 + e);  // sigma(x)
     const double below = x >= 0 ? e / (1.0 + e) : 1.0 / (1.0 + e);  // sigma(-x)
-    slope_of = a.scale * a.beta * (a.smoothing * above - (1.0 - a.smoothing) * below);
+    slope_of = a.grad_scale * a.beta * (a.smoothing * above - (1.0 - a.smoothing) * below);
   }
   __syncthreads();
   const double slope = slope_of;
@@ -539,7 +538,7 @@ struct Workspace {  // a counter; per row a partial loss, the log-probability, w
   double *part, *logp;
   float *top, *inv, *coef;
 };
-size_t workspace_bytes(int rows, int pairs) {
+size_t scratch_bytes(int rows, int pairs) {
   const size_t n = (size_t)(rows > pairs ? rows : pairs);
   return n * sizeof(double) + (size_t)rows * (sizeof(double) + 3 * sizeof(float)) + 256;
 }
@@ -613,6 +612,68 @@ hipError_t launch_grad(const zb_logits* x, const Rows& of, const float* coef, co
 zb_status said(hipError_t e) { return e == hipSuccess ? ZB_OK : ZB_EDEVICE; }
 
 }  // namespace
+
+size_t loss_workspace_bytes(int rows, int pairs) { return scratch_bytes(rows, pairs); }
+
+bool valid_policy(const zb_policy* p) {
+  return p->clip_low >= 0 && p->clip_low <= 1 && p->clip_high >= 0 && p->kl_coef >= 0 && isfinite(p->clip_high) && isfinite(p->kl_coef) && isfinite(p->scale);
+}
+bool valid_preference(const zb_preference* p) {
+  return p->pairs >= 0 && p->pairs <= kMaxRows && isfinite(p->beta) && isfinite(p->scale) && p->label_smoothing >= 0 && p->label_smoothing <= 1;
+}
+
+zb_status policy_loss(const zb_logits* x, const zb_policy* p, double grad_scale, float* loss, float* logp, void* dlogits, int64_t dlogits_stride,
+                      void* workspace, size_t workspace_size, hipStream_t s) {
+  if (!valid_logits(x) || !p || !loss || !valid_dlogits(x, dlogits, &dlogits_stride) || !valid_policy(p)) return ZB_EINVAL;
+  if (x->rows && (!p->old_logp || !p->advantage || (p->kl_coef != 0 && !p->ref_logp))) return ZB_EINVAL;
+  if (!workspace || misaligned(workspace, 8) || workspace_size < scratch_bytes(x->rows, 0)) return ZB_EINVAL;
+  if (misaligned(loss, 4) || misaligned(logp, 4) || misaligned(p->old_logp, 4) || misaligned(p->advantage, 4) || misaligned(p->ref_logp, 4) ||
+      misaligned(p->weight, 4))
+    return ZB_EINVAL;
+  OnDeviceOf on(s);
+  if (!on.ok) return ZB_EDEVICE;
+  const Workspace w = carve(workspace, x->rows, 0);
+  if (x->rows) {
+    const Rows of{x->targets, p->weight, nullptr, 0, x->vocab};
+    const PolicyArgs a{p->old_logp, p->ref_logp, p->advantage, 1.0 - p->clip_low, 1.0 + p->clip_high, log(1.0 - p->clip_low), log1p(p->clip_high), p->kl_coef, p->scale, grad_scale};
+    RowOut out{logp};
+    out.part = w.part;
+    if (x->rows <= kSumInPlace) out.total = Total{loss, w.done};
+    const hipError_t e = x->dtype == ZB_BF16 ? launch_policy<bf16_t>(x, of, out, a, dlogits, dlogits_stride, s)
+                                             : launch_policy<float>(x, of, out, a, dlogits, dlogits_stride, s);
+    if (e != hipSuccess || out.total.loss) return said(e);
+  }
+  sum_kernel<<<1, 1024, 0, s>>>(w.part, x->rows, loss);
+  return said(hipGetLastError());
+}
+
+zb_status preference_loss(const zb_logits* x, const zb_preference* p, double grad_scale, float* loss, float* logp, float* rewards, void* dlogits,
+                          int64_t dlogits_stride, void* workspace, size_t workspace_size, hipStream_t s) {
+  if (!valid_logits(x) || !p || !loss || !valid_dlogits(x, dlogits, &dlogits_stride) || !valid_preference(p)) return ZB_EINVAL;
+  if ((p->pairs && !p->offsets) || (x->rows && p->pairs && !p->ref_logp)) return ZB_EINVAL;
+  if (!workspace || misaligned(workspace, 8) || workspace_size < scratch_bytes(x->rows, p->pairs)) return ZB_EINVAL;
+  if (misaligned(loss, 4) || misaligned(logp, 4) || misaligned(rewards, 4) || misaligned(p->offsets, 4) || misaligned(p->ref_logp, 4) ||
+      misaligned(p->weight, 4))
+    return ZB_EINVAL;
+  OnDeviceOf on(s);
+  if (!on.ok) return ZB_EDEVICE;
+  const Workspace w = carve(workspace, x->rows, p->pairs);
+  const Rows of{x->targets, p->weight, p->pairs ? p->offsets : nullptr, p->pairs ? 2 * p->pairs : -1, x->vocab};
+  if (x->rows) {
+    RowOut out{logp};
+    out.top = w.top; out.inv = w.inv; out.logp64 = w.logp;
+    if (launch_logp(x, of, out, s) != hipSuccess) return ZB_EDEVICE;
+  }
+  if (p->pairs) {
+    const PairArgs a{p->ref_logp, p->beta, p->label_smoothing, p->scale, grad_scale};
+    pair_kernel<<<p->pairs, kThreads, 0, s>>>(a, of, x->rows, w.logp, rewards, w.coef, w.part, p->pairs <= kSumInPlace ? Total{loss, w.done} : Total{});
+    if (hipGetLastError() != hipSuccess) return ZB_EDEVICE;
+  }
+  if (x->rows && dlogits && launch_grad(x, of, w.coef, w.top, w.inv, dlogits, dlogits_stride, s) != hipSuccess) return ZB_EDEVICE;
+  if (!p->pairs || p->pairs > kSumInPlace) sum_kernel<<<1, 1024, 0, s>>>(w.part, p->pairs, loss);
+  return said(hipGetLastError());
+}
+
 }  // namespace zb
 
 using namespace zb;
@@ -639,67 +700,18 @@ zb_status zb_token_logprobs_backward(const zb_logits* x, const float* lse, const
 
 zb_status zb_loss_workspace_bytes(int32_t rows, int32_t pairs, size_t* bytes) {
   if (!bytes || rows < 0 || rows > kMaxRows || pairs < 0 || pairs > kMaxRows) return ZB_EINVAL;
-  *bytes = workspace_bytes(rows, pairs);
+  *bytes = loss_workspace_bytes(rows, pairs);
   return ZB_OK;
 }
 
 zb_status zb_policy_loss(const zb_logits* x, const zb_policy* p, float* loss, float* logp, void* dlogits, int64_t dlogits_stride,
                          void* workspace, size_t workspace_size, void* hip_stream) {
-  if (!valid_logits(x) || !p || !loss || !valid_dlogits(x, dlogits, &dlogits_stride)) return ZB_EINVAL;
-  if (!(p->clip_low >= 0 && p->clip_low <= 1 && p->clip_high >= 0 && p->kl_coef >= 0) || !isfinite(p->clip_high) ||
-      !isfinite(p->kl_coef) || !isfinite(p->scale))
-    return ZB_EINVAL;
-  if (x->rows && (!p->old_logp || !p->advantage || (p->kl_coef != 0 && !p->ref_logp))) return ZB_EINVAL;
-  if (!workspace || misaligned(workspace, 8) || workspace_size < workspace_bytes(x->rows, 0)) return ZB_EINVAL;
-  if (misaligned(loss, 4) || misaligned(logp, 4) || misaligned(p->old_logp, 4) || misaligned(p->advantage, 4) || misaligned(p->ref_logp, 4) ||
-      misaligned(p->weight, 4))
-    return ZB_EINVAL;
-  const hipStream_t s = (hipStream_t)hip_stream;
-  OnDeviceOf on(s);
-  if (!on.ok) return ZB_EDEVICE;
-  const Workspace w = carve(workspace, x->rows, 0);
-  if (x->rows) {
-    const Rows of{x->targets, p->weight, nullptr, 0, x->vocab};
-    const PolicyArgs a{p->old_logp, p->ref_logp, p->advantage, 1.0 - p->clip_low, 1.0 + p->clip_high, log(1.0 - p->clip_low), log1p(p->clip_high), p->kl_coef, p->scale};
-    RowOut out{logp};
-    out.part = w.part;
-    if (x->rows <= kSumInPlace) out.total = Total{loss, w.done};
-    const hipError_t e = x->dtype == ZB_BF16 ? launch_policy<bf16_t>(x, of, out, a, dlogits, dlogits_stride, s)
-                                             : launch_policy<float>(x, of, out, a, dlogits, dlogits_stride, s);
-    if (e != hipSuccess || out.total.loss) return said(e);
-  }
-  sum_kernel<<<1, 1024, 0, s>>>(w.part, x->rows, loss);
-  return said(hipGetLastError());
+  return policy_loss(x, p, p ? p->scale : 0.0, loss, logp, dlogits, dlogits_stride, workspace, workspace_size, (hipStream_t)hip_stream);
 }
 
 zb_status zb_preference_loss(const zb_logits* x, const zb_preference* p, float* loss, float* logp, float* rewards, void* dlogits,
                              int64_t dlogits_stride, void* workspace, size_t workspace_size, void* hip_stream) {
-  if (!valid_logits(x) || !p || !loss || !valid_dlogits(x, dlogits, &dlogits_stride)) return ZB_EINVAL;
-  if (p->pairs < 0 || p->pairs > kMaxRows || !isfinite(p->beta) || !isfinite(p->scale) || !(p->label_smoothing >= 0 && p->label_smoothing <= 1))
-    return ZB_EINVAL;
-  if ((p->pairs && !p->offsets) || (x->rows && p->pairs && !p->ref_logp)) return ZB_EINVAL;
-  if (!workspace || misaligned(workspace, 8) || workspace_size < workspace_bytes(x->rows, p->pairs)) return ZB_EINVAL;
-  if (misaligned(loss, 4) || misaligned(logp, 4) || misaligned(rewards, 4) || misaligned(p->offsets, 4) || misaligned(p->ref_logp, 4) ||
-      misaligned(p->weight, 4))
-    return ZB_EINVAL;
-  const hipStream_t s = (hipStream_t)hip_stream;
-  OnDeviceOf on(s);
-  if (!on.ok) return ZB_EDEVICE;
-  const Workspace w = carve(workspace, x->rows, p->pairs);
-  const Rows of{x->targets, p->weight, p->pairs ? p->offsets : nullptr, p->pairs ? 2 * p->pairs : -1, x->vocab};
-  if (x->rows) {
-    RowOut out{logp};
-    out.top = w.top; out.inv = w.inv; out.logp64 = w.logp;
-    if (launch_logp(x, of, out, s) != hipSuccess) return ZB_EDEVICE;
-  }
-  if (p->pairs) {
-    const PairArgs a{p->ref_logp, p->beta, p->label_smoothing, p->scale};
-    pair_kernel<<<p->pairs, kThreads, 0, s>>>(a, of, x->rows, w.logp, rewards, w.coef, w.part, p->pairs <= kSumInPlace ? Total{loss, w.done} : Total{});
-    if (hipGetLastError() != hipSuccess) return ZB_EDEVICE;
-  }
-  if (x->rows && dlogits && launch_grad(x, of, w.coef, w.top, w.inv, dlogits, dlogits_stride, s) != hipSuccess) return ZB_EDEVICE;
-  if (!p->pairs || p->pairs > kSumInPlace) sum_kernel<<<1, 1024, 0, s>>>(w.part, p->pairs, loss);
-  return said(hipGetLastError());
+  return preference_loss(x, p, p ? p->scale : 0.0, loss, logp, rewards, dlogits, dlogits_stride, workspace, workspace_size, (hipStream_t)hip_stream);
 }
 
 }  // extern "C"

@@ -133,3 +133,27 @@ def test_bad_arguments_of_the_norm_and_of_moving_moments():
     assert zb.lib.zb_adamw_workspace_bytes(t, 1, None) == zb.EINVAL
     assert zb.lib.zb_adamw_read_moments(t, 1, None, None) == zb.EINVAL
     assert C.sizeof(zb.binding.zb_adamw_tensor) == 80
+
+
+def test_loss_configurations_of_a_stage():
+    nan, inf = float("nan"), float("inf")
+
+    def rc(**k):
+        cfg = zb.binding.zb_config()
+        zb.lib.zb_config_defaults(C.byref(cfg))
+        assert (cfg.loss, cfg.clip_low, cfg.clip_high, cfg.kl_coef, cfg.pref_beta, cfg.label_smoothing) == (0, 0.2, 0.2, 0.0, 0.1, 0.0)
+        base = dict(layers=1, hidden=64, heads=2, ffn=256, seq=32, mb_size=2, max_microbatches=2, max_pending_b=2, max_pending_w=2, max_inflight=3, role=2,
+                    vocab=512)
+        for name, value in {**base, **k}.items():
+            setattr(cfg, name, value)
+        need = C.c_size_t(0)
+        return zb.lib.zb_stage_arena_bytes(C.byref(cfg), C.byref(need)), need.value
+
+    plain, policy, pairs = rc()[1], rc(loss=1), rc(loss=2)
+    assert policy[0] == pairs[0] == zb.OK
+    # the gradient takes the logits' place: three stashes of [64, 512] instead of two of logits and two of gradients, beside a few floats a token
+    assert policy[1] < plain and pairs[1] < plain
+    for bad in (dict(loss=3), dict(loss=-1), dict(loss=1, role=0), dict(loss=2, role=1), dict(loss=2, mb_size=3), dict(loss=1, clip_low=-0.1),
+                dict(loss=1, clip_low=1.5), dict(loss=1, clip_high=inf), dict(loss=1, kl_coef=-1.0), dict(loss=1, kl_coef=nan), dict(loss=2, pref_beta=inf),
+                dict(loss=2, label_smoothing=1.5), dict(loss=2, label_smoothing=nan)):
+        assert rc(**bad)[0] == zb.EINVAL, bad

@@ -101,3 +101,56 @@ def test_adamw_step_is_the_stages_step():
     got = A.step(th, g, m, v, 5, lr=1e-3, beta1=hp.beta1, beta2=hp.beta2, eps=hp.eps, decay=hp.weight_decay, coef=1.0)
     for a, b in zip(got, (st.theta, st.m, st.v)):
         assert np.allclose(a, b, rtol=1e-12, atol=0)
+
+
+@pytest.mark.parametrize("kind", ["policy", "preference"])
+def test_loss_stage_gradients_against_differences(kind):
+    """The head's, the final LayerNorm's and the input's gradients of the mean loss over two microbatches."""
+    import zb_inputs
+    w = zb_inputs.Workload("loss", "fp32", 1, 16, 2, 32, 5, 2, 2, 1, 2, "H1", seed=5)
+    vocab, m = 13, 2
+    rng = np.random.default_rng(9)
+    X = [rng.normal(size=(10, 16)) for _ in range(m)]
+    t = [rng.integers(0, vocab, 10) for _ in range(m)]
+    weight = [rng.uniform(0.5, 1.5, 10) * (np.arange(10) != 3) for _ in range(m)]
+    shift = [np.resize([0.0, 0.6, -0.7, 0.05], 10) for _ in range(m)]   # ratios far from the borders
+    ref, adv = [rng.normal(0, 0.3, 10) for _ in range(m)], [rng.normal(size=10) for _ in range(m)]
+    base = zb_inputs.end_stage_params(w, "last", vocab)
+    base["w_head"] = base["w_head"] * 30
+    params, logp0 = zb_inputs.stage_params(w), {}
+
+    def run(extra, x0, backward=False):
+        o = L.LossStageOracle(kind=kind, low=0.2, high=0.3, kl=0.1, beta=0.4, eps=0.1, vocab=vocab, extra_params=extra, layers=1, hidden=16, heads=2,
+                              ffn=32, seq=5, mb_size=2, dtype="fp32", params=params)
+        o.begin_iteration(m)
+        for k in range(m):
+            o.set_input(k, x0 if k == 0 else X[k])
+            o.set_targets(k, t[k])
+            lp = logp0.get(k, np.zeros(10))
+            o.set_values(k, weight=weight[k], old=lp + shift[k], advantage=adv[k], ref=lp + ref[k])
+            o.forward(k)
+        if backward:
+            for k in range(m):
+                o.backward_input(k)
+                o.backward_weight(k)
+        return o
+
+    for k, lp in run(base, X[0]).logp.items():
+        logp0[k] = lp
+    o = run(base, X[0], backward=True)
+
+    def difference(change, h=1e-6):
+        return (change(h) - change(-h)) / (2 * h)
+
+    for name, at in (("w_head", (3, 4)), ("w_head", (10, int(t[0][1]))), ("lnf_g", (5,)), ("lnf_b", (2,))):
+        def change(h):
+            e = {k: v.astype(np.float64).copy() for k, v in base.items()}
+            e[name][at] += h
+            return run(e, X[0]).iteration_loss()
+        assert np.isclose(difference(change), o.grads[o.nl][name][at], rtol=1e-5, atol=1e-9), name
+    for at in ((0, 0), (6, 9)):
+        def change(h):
+            x = X[0].copy()
+            x[at] += h
+            return run(base, x).iteration_loss()
+        assert np.isclose(difference(change), o.dX[0][at], rtol=1e-5, atol=1e-9)
