@@ -404,15 +404,16 @@ __global__ __launch_bounds__(THREADS) void row_kernel(const T* logits, long stri
   if (POLICY) add_to_total<THREADS>(out.total, out.part, loss);
 }
 
-// coef ([j = target] - exp(z_j - top) inv), inv null: 1, by workgroups of kThreads * kGradVectors vectors of a row; rows from the
-// last to the first: the last ones read are the likeliest to lie in a cache still
-constexpr int kGradVectors = 4;
+// coef ([j = target] - exp(z_j - top) inv), inv null: 1, by workgroups of kThreads * kGradVectors vectors of a row (us of 5513 rows
+// of 50432 bf16 after their log-probabilities with 2 / 4 / 8 vectors a lane: 236 / 239 / 258; from the last row to the first, towards what the
+// caches may still hold: 239)
+constexpr int kGradVectors = 2;
 template <typename T, bool NT>
 __global__ __launch_bounds__(kThreads) void grad_kernel(const T* logits, long stride, Rows of, const float* __restrict__ coefs,
                                                         const float* __restrict__ tops, const float* __restrict__ invs, T* dlogits, long dstride,
-                                                        int parts, int rows) {
+                                                        int parts) {
   constexpr int VE = Span<T>::VE;
-  const int from_last = blockIdx.x / parts, row = rows - 1 - from_last, part = blockIdx.x - from_last * parts, lane = threadIdx.x;
+  const int row = blockIdx.x / parts, part = blockIdx.x - row * parts, lane = threadIdx.x;
   const float coef = of.counts(row) ? coefs[row] : 0.f;
   const T* z = logits + (long)row * stride;
   T* d = dlogits + (long)row * dstride;
@@ -484,15 +485,18 @@ __device__ __forceinline__ void sequence_rows(const int* offsets, int q, int row
 }
 
 // One workgroup per pair: both sequences' sums of w (logp - ref), the pair's loss, and the coefficient of every row.
-__global__ __launch_bounds__(kThreads) void pair_kernel(PairArgs a, Rows of, int rows, const double* __restrict__ logp, float* __restrict__ rewards,
-                                                        float* __restrict__ coef, double* part, Total total) {
-  __shared__ double red[2][kThreads / 64], slope_of;
+constexpr int kPairThreads = 1024;
+__global__ __launch_bounds__(kPairThreads) void pair_kernel(PairArgs a, Rows of, int rows, const double* __restrict__ logp, float* __restrict__ rewards,
+                                                            float* __restrict__ coef, double* part, Total total) {
+  __shared__ double red[2][kPairThreads / 64], slope_of;
   int lo[2], hi[2];
   for (int q = 0; q < 2; ++q) {
     sequence_rows(of.offsets, 2 * blockIdx.x + q, rows, &lo[q], &hi[q]);
     double acc = 0.0;
-    for (int r = lo[q] + threadIdx.x; r < hi[q]; r += kThreads)
-      if (of.counts(r)) acc += of.weight_of(r) * (logp[r] - (double)a.ref_logp[r]);
+    for (int r = lo[q] + threadIdx.x; r < hi[q]; r += kPairThreads) {
+      const double gap = logp[r] - (double)a.ref_logp[r];  // (whatever a row that does not count holds there)
+      if (of.counts(r)) acc += of.weight_of(r) * gap;
+    }
     acc = wave_sum(acc);
     if ((threadIdx.x & 63) == 0) red[q][threadIdx.x >> 6] = acc;
   }
@@ -502,7 +506,7 @@ __global__ __launch_bounds__(kThreads) void pair_kernel(PairArgs a, Rows of, int
     double s[2];
     for (int q = 0; q < 2; ++q) {
       s[q] = red[q][0];
-      for (int w = 1; w < kThreads / 64; ++w) s[q] += red[q][w];
+      for (int w = 1; w < kPairThreads / 64; ++w) s[q] += red[q][w];
       if (rewards) rewards[2 * blockIdx.x + q] = (float)(a.beta * s[q]);
     }
     const double x = a.beta * (s[0] - s[1]), e = exp(-fabs(x)), l = log1p(e);  // -log sigma(x) = max(-x, 0) + l
@@ -514,8 +518,8 @@ __global__ __launch_bounds__(kThreads) void pair_kernel(PairArgs a, Rows of, int
   __syncthreads();
   const double slope = slope_of;
   for (int q = 0; q < 2; ++q)
-    for (int r = lo[q] + threadIdx.x; r < hi[q]; r += kThreads) coef[r] = (float)((q ? -slope : slope) * of.weight_of(r));
-  add_to_total<kThreads>(total, part, loss);
+    for (int r = lo[q] + threadIdx.x; r < hi[q]; r += kPairThreads) coef[r] = (float)((q ? -slope : slope) * of.weight_of(r));
+  add_to_total<kPairThreads>(total, part, loss);
 }
 
 constexpr int kMaxRows = 1 << 24;
@@ -564,19 +568,26 @@ bool past_caches(const zb_logits* x) { return (size_t)x->rows * x->vocab * (x->d
     else { constexpr bool NT = false; call; }                                \
   } while (0)
 
-template <typename T> hipError_t launch_logp(const zb_logits* x, const Rows& of, const RowOut& out, hipStream_t s) {
+// last: nothing reads the logits again
+template <typename T> hipError_t launch_logp(const zb_logits* x, const Rows& of, const RowOut& out, bool last, hipStream_t s) {
   const int vectors = x->vocab / Span<T>::VE;
-#define ZB_ROWS(THREADS, U)                                                                                                                   \
-  ZB_NT((row_kernel<T, THREADS, U, false, NT><<<x->rows, THREADS, 0, s>>>((const T*)x->logits, x->row_stride, of, out, PolicyArgs{}, (T*)nullptr, 0)))
+#define ZB_LOGP(THREADS, U, NT) \
+  row_kernel<T, THREADS, U, false, NT><<<x->rows, THREADS, 0, s>>>((const T*)x->logits, x->row_stride, of, out, PolicyArgs{}, (T*)nullptr, 0)
+#define ZB_ROWS(THREADS, U)                                    \
+  do {                                                         \
+    if (last && past_caches(x)) ZB_LOGP(THREADS, U, true);     \
+    else ZB_LOGP(THREADS, U, false);                           \
+  } while (0)
   if (vectors <= 512) ZB_ROWS(64, 4);
   else if (vectors <= 2048) ZB_ROWS(256, 4);
   else if (x->rows >= 512) ZB_ROWS(512, 4);
   else ZB_ROWS(1024, 2);
 #undef ZB_ROWS
+#undef ZB_LOGP
   return hipGetLastError();
 }
-hipError_t launch_logp(const zb_logits* x, const Rows& of, const RowOut& out, hipStream_t s) {
-  return x->dtype == ZB_BF16 ? launch_logp<bf16_t>(x, of, out, s) : launch_logp<float>(x, of, out, s);
+hipError_t launch_logp(const zb_logits* x, const Rows& of, const RowOut& out, bool last, hipStream_t s) {
+  return x->dtype == ZB_BF16 ? launch_logp<bf16_t>(x, of, out, last, s) : launch_logp<float>(x, of, out, last, s);
 }
 
 template <typename T>
@@ -603,7 +614,7 @@ template <typename T>
 hipError_t launch_grad(const zb_logits* x, const Rows& of, const float* coef, const float* top, const float* inv, void* d, int64_t stride, hipStream_t s) {
   const int per = kThreads * kGradVectors, vectors = x->vocab / Span<T>::VE, parts = vectors > per ? (vectors + per - 1) / per : 1;
   ZB_NT((grad_kernel<T, NT><<<(unsigned)x->rows * (unsigned)parts, kThreads, 0, s>>>((const T*)x->logits, x->row_stride, of, coef, top, inv, (T*)d,
-                                                                                     stride, parts, x->rows)));
+                                                                                     stride, parts)));
   return hipGetLastError();
 }
 hipError_t launch_grad(const zb_logits* x, const Rows& of, const float* coef, const float* top, const float* inv, void* d, int64_t stride, hipStream_t s) {
@@ -662,11 +673,11 @@ zb_status preference_loss(const zb_logits* x, const zb_preference* p, double gra
   if (x->rows) {
     RowOut out{logp};
     out.top = w.top; out.inv = w.inv; out.logp64 = w.logp;
-    if (launch_logp(x, of, out, s) != hipSuccess) return ZB_EDEVICE;
+    if (launch_logp(x, of, out, dlogits == nullptr, s) != hipSuccess) return ZB_EDEVICE;
   }
   if (p->pairs) {
     const PairArgs a{p->ref_logp, p->beta, p->label_smoothing, p->scale, grad_scale};
-    pair_kernel<<<p->pairs, kThreads, 0, s>>>(a, of, x->rows, w.logp, rewards, w.coef, w.part, p->pairs <= kSumInPlace ? Total{loss, w.done} : Total{});
+    pair_kernel<<<p->pairs, kPairThreads, 0, s>>>(a, of, x->rows, w.logp, rewards, w.coef, w.part, p->pairs <= kSumInPlace ? Total{loss, w.done} : Total{});
     if (hipGetLastError() != hipSuccess) return ZB_EDEVICE;
   }
   if (x->rows && dlogits && launch_grad(x, of, w.coef, w.top, w.inv, dlogits, dlogits_stride, s) != hipSuccess) return ZB_EDEVICE;
@@ -685,7 +696,7 @@ zb_status zb_token_logprobs(const zb_logits* x, float* logp, float* lse, void* h
   if (x->rows == 0) return ZB_OK;
   OnDeviceOf on((hipStream_t)hip_stream);
   if (!on.ok) return ZB_EDEVICE;
-  return said(launch_logp(x, Rows{x->targets, nullptr, nullptr, 0, x->vocab}, RowOut{logp, lse}, (hipStream_t)hip_stream));
+  return said(launch_logp(x, Rows{x->targets, nullptr, nullptr, 0, x->vocab}, RowOut{logp, lse}, true, (hipStream_t)hip_stream));
 }
 
 zb_status zb_token_logprobs_backward(const zb_logits* x, const float* lse, const float* dlogp, void* dlogits, int64_t dlogits_stride,
