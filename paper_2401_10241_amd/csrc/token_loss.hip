@@ -133,19 +133,24 @@ struct PolicyArgs {
 };
 // exp(d) to the last bit or two of fp32, whatever the size of d
 __device__ __forceinline__ double exp_near(double d) {
-  const float h = (float)d, l = (float)(d - (double)h);
-  const float e = expf(h);
-  return (double)e + (e < INFINITY ? (double)(e * l) : 0.0);
+  const float h = (float)d, e = expf(h);
+  return e > 0.f && e < INFINITY ? (double)e + (double)(e * (float)(d - (double)h)) : (double)e;
 }
-// exp(d) - d - 1; the digits that the subtraction would take near 0 come from the series
-__device__ __forceinline__ double exp_above_line(double d) {
-  if (fabs(d) > 1.0) return exp_near(d) - d - 1.0;
+// exp(d) - d - 1, and exp(d) - 1 in *up; the digits that the subtractions would take near 0 come from the series
+__device__ __forceinline__ double exp_above_line(double d, double* up) {
+  if (!(fabs(d) <= 1.0)) {
+    const double e = exp_near(d);
+    *up = e - 1.0;
+    return e < INFINITY ? e - d - 1.0 : e;
+  }
   const float x = (float)d;
   float t = 1.0f / 39916800.0f;  // 1 / 11!
   t = fmaf(t, x, 1.0f / 3628800.0f); t = fmaf(t, x, 1.0f / 362880.0f); t = fmaf(t, x, 1.0f / 40320.0f); t = fmaf(t, x, 1.0f / 5040.0f);
   t = fmaf(t, x, 1.0f / 720.0f); t = fmaf(t, x, 1.0f / 120.0f); t = fmaf(t, x, 1.0f / 24.0f); t = fmaf(t, x, 1.0f / 6.0f);
   t = fmaf(t, x, 0.5f);
-  return d * d * (double)t;
+  const double k = d * d * (double)t;
+  *up = k + d;
+  return k;
 }
 // Loss of a row and its derivative by the row's log-probability.  One lane does this while the others wait, so it takes the
 // exponential of fp32; what is compared with a border is the logarithm, in 64 bits.
@@ -156,9 +161,9 @@ __device__ __forceinline__ double policy_row(const PolicyArgs& a, const Rows& of
   double loss = -fmin(rho * adv, held * adv);
   double g = (adv > 0 && above) || (adv < 0 && below) ? 0.0 : -adv * rho;
   if (a.kl != 0.0) {
-    const double d = (double)a.ref_logp[row] - logp, k = exp_above_line(d);
-    loss += a.kl * k;
-    g -= a.kl * (k + d);
+    double up;
+    loss += a.kl * exp_above_line((double)a.ref_logp[row] - logp, &up);
+    g -= a.kl * up;
   }
   *slope = a.grad_scale * w * g;
   return a.scale * w * loss;
@@ -613,6 +618,7 @@ hipError_t launch_policy(const zb_logits* x, const Rows& of, const RowOut& out, 
 template <typename T>
 hipError_t launch_grad(const zb_logits* x, const Rows& of, const float* coef, const float* top, const float* inv, void* d, int64_t stride, hipStream_t s) {
   const int per = kThreads * kGradVectors, vectors = x->vocab / Span<T>::VE, parts = vectors > per ? (vectors + per - 1) / per : 1;
+  if ((int64_t)x->rows * parts > 0x7FFFFFFF) return hipErrorInvalidValue;  // (more logits than any memory holds)
   ZB_NT((grad_kernel<T, NT><<<(unsigned)x->rows * (unsigned)parts, kThreads, 0, s>>>((const T*)x->logits, x->row_stride, of, coef, top, inv, (T*)d,
                                                                                      stride, parts)));
   return hipGetLastError();

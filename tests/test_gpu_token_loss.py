@@ -345,6 +345,35 @@ def test_large_ratios_and_far_references():
     assert host(loss)[0] == np.inf and not g[0].any() and np.abs(g[1]).max() < 1e-38 and g[2, k.targets[2]] == np.inf
 
 
+def test_targets_that_the_policy_or_the_reference_rules_out():
+    """log-probabilities of -infinity: the ratio is 0, the KL term infinite where the reference allows the token, and no NaN beside them."""
+    import torch
+    import paper_2401_10241_amd as zb
+    k = Case("fp32", 4, 50)
+    k.targets[:] = 7
+    k.z[0, 7] = k.z[1, 7] = -float("inf")
+    k.place()
+    lp = L.logprobs(k.z64, k.targets)[0]
+    old, ref = np.full(4, -3.0, np.float32), np.full(4, -3.0, np.float32)
+    old[2:] = lp[2:]
+    ref[3] = -np.inf
+    for adv in (1.0, -1.0):
+        keep = dev(old), dev(np.full(4, adv, np.float32)), dev(ref)
+        for kl in (0.0, 0.1):
+            loss, ws = torch.zeros(1, device="cuda"), scratch(4)
+            zb.policy_loss(k.x(), zb.policy(keep[0].data_ptr(), keep[1].data_ptr(), ref_logp=keep[2].data_ptr(), clip_low=0.2, clip_high=0.3, kl_coef=kl),
+                           loss.data_ptr(), 0, k.dflat.data_ptr(), workspace=ws.data_ptr(), workspace_bytes=ws.numel())
+            g = k.gradient()
+            # rho = 0: -min(0, 0.8 A) is 0 for a gain, 0.8 |A| for a loss, neither with a gradient
+            each = 0.0 if adv > 0 else 0.8
+            if kl == 0:
+                assert abs(host(loss)[0] - (2 * each - 2 * adv)) <= 1e-5 and not g[:2].any() and np.isfinite(g).all()
+            else:
+                assert host(loss)[0] == np.inf and np.isfinite(g[2:]).all() and g[0, 7] == -np.inf
+                # reference -infinity: d(exp(d) - d - 1)/dlogp = 1 - exp(d) = 1
+                assert abs(g[3, 7] - (kl - adv) * (1 - np.exp(lp[3]))) <= 1e-5
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 def test_captured_losses_replay_like_eager_ones(dtype):
     """Captured on a side stream and replayed with new logits each time, eager work between the replays."""
