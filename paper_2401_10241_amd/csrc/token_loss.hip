@@ -73,13 +73,34 @@ template <int NV> __device__ __forceinline__ void as_loaded(uint4 (&r)[NV]) {
 }
 
 __device__ __forceinline__ float exp_of(float x, float top) { return __builtin_amdgcn_exp2f((x - top) * kLog2e); }
-// log(s) of 1 <= s < 2^19 (or NaN), off by 3e-8: the exponent apart, so that no digits go to it
-__device__ __forceinline__ double log_of(float s) {
-  const int e = (int)(__float_as_uint(s) >> 23) - 127;
-  const float f = __uint_as_float((__float_as_uint(s) & 0x007FFFFFu) | 0x3F800000u);
-  const bool up = f > 1.41421356f;
-  const double l = (double)(e + (up ? 1 : 0)) + (double)__builtin_amdgcn_logf(up ? 0.5f * f : f);
-  return s == s ? l * 0.6931471805599453 : (double)s;
+// The same for sums over a row, without the bias of a log2(e) of 24 bits: log-probabilities are added over sequences, where errors of one sign
+// would add up while the values cancel.
+__device__ __forceinline__ float exp_for_sum(float x, float top) {
+  const float d = x - top;
+  return __builtin_amdgcn_exp2f(fmaf(d, kLog2e, d * 1.925963033e-8f));
+}
+// Sum of a vector's exponentials.  Vectors are added up in 64 bits: one large term would round off a part of each small one that follows it.
+template <int VE> __device__ __forceinline__ double exp_sum(const float (&x)[VE], float top) {
+  float t[VE];
+#pragma unroll
+  for (int e = 0; e < VE; ++e) t[e] = exp_for_sum(x[e], top);
+#pragma unroll
+  for (int w = VE / 2; w > 0; w /= 2)
+#pragma unroll
+    for (int e = 0; e < w; ++e) t[e] += t[e + w];
+  return (double)t[0];
+}
+// log(s) of 1 <= s < 2^19 (or NaN): the exponent apart, the rest from 2 atanh(z), z = (f - 1) / (f + 1), |z| < 0.172, to 1e-12
+__device__ __forceinline__ double log_of(double s) {
+  const unsigned high = (unsigned)__double2hiint(s);
+  int e = (int)(high >> 20) - 1023;
+  double f = __hiloint2double((int)((high & 0x000FFFFFu) | 0x3FF00000u), __double2loint(s));
+  if (f > 1.41421356) { f *= 0.5; ++e; }
+  const double z = (f - 1.0) / (f + 1.0), q = z * z;
+  double t = 1.0 / 15.0;
+  t = fma(t, q, 1.0 / 13.0); t = fma(t, q, 1.0 / 11.0); t = fma(t, q, 1.0 / 9.0); t = fma(t, q, 1.0 / 7.0); t = fma(t, q, 1.0 / 5.0);
+  t = fma(t, q, 1.0 / 3.0);
+  return s == s ? fma((double)e, 0.6931471805599453, 2.0 * fma(z * q, t, z)) : s;
 }
 
 // what the lanes of a workgroup of N waves hold, reduced in a fixed order; `red` is read after the barrier only
@@ -93,7 +114,7 @@ template <int N> __device__ __forceinline__ float block_max(float v, float* red)
   for (int w = 1; w < N; ++w) v = fmaxf(v, red[w]);
   return v;
 }
-template <int N> __device__ __forceinline__ float block_sum(float v, float* red) {
+template <int N> __device__ __forceinline__ double block_sum(double v, double* red) {
   v = wave_sum(v);
   if (N == 1) return v;
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
@@ -131,29 +152,32 @@ struct PolicyArgs {
   const float *old_logp, *ref_logp, *advantage;
   double lo, hi, log_lo, log_hi, kl, scale, grad_scale;  // borders of the ratio and of its logarithm
 };
-// exp(d) to the last bit or two of fp32, whatever the size of d
+// exp(d), off by 1e-11 of it: 2^k e^r with |r| <= log(2) / 2 and nine terms of the series, a chain that one lane runs in a few hundred
+// cycles.  (Advantages have both signs: the sum of the rows' losses is far smaller than the losses, so 32 bits are not enough here.)
 __device__ __forceinline__ double exp_near(double d) {
-  const float h = (float)d, e = expf(h);
-  return e > 0.f && e < INFINITY ? (double)e + (double)(e * (float)(d - (double)h)) : (double)e;
+  if (!(fabs(d) < 700.0)) return d > 0.0 ? (double)INFINITY : d < 0.0 ? 0.0 : d;
+  const double k = rint(d * 1.4426950408889634);
+  const double r = fma(k, -0.6931471805599453, d);
+  double t = 1.0 / 362880.0;
+  t = fma(t, r, 1.0 / 40320.0); t = fma(t, r, 1.0 / 5040.0); t = fma(t, r, 1.0 / 720.0); t = fma(t, r, 1.0 / 120.0);
+  t = fma(t, r, 1.0 / 24.0); t = fma(t, r, 1.0 / 6.0); t = fma(t, r, 0.5); t = fma(t, r, 1.0); t = fma(t, r, 1.0);
+  return ldexp(t, (int)k);
 }
 // exp(d) - d - 1, and exp(d) - 1 in *up; the digits that the subtractions would take near 0 come from the series
 __device__ __forceinline__ double exp_above_line(double d, double* up) {
-  if (!(fabs(d) <= 1.0)) {
+  if (!(fabs(d) <= 0.5)) {
     const double e = exp_near(d);
     *up = e - 1.0;
     return e < INFINITY ? e - d - 1.0 : e;
   }
-  const float x = (float)d;
-  float t = 1.0f / 39916800.0f;  // 1 / 11!
-  t = fmaf(t, x, 1.0f / 3628800.0f); t = fmaf(t, x, 1.0f / 362880.0f); t = fmaf(t, x, 1.0f / 40320.0f); t = fmaf(t, x, 1.0f / 5040.0f);
-  t = fmaf(t, x, 1.0f / 720.0f); t = fmaf(t, x, 1.0f / 120.0f); t = fmaf(t, x, 1.0f / 24.0f); t = fmaf(t, x, 1.0f / 6.0f);
-  t = fmaf(t, x, 0.5f);
-  const double k = d * d * (double)t;
+  double t = 1.0 / 39916800.0;  // 1 / 11!
+  t = fma(t, d, 1.0 / 3628800.0); t = fma(t, d, 1.0 / 362880.0); t = fma(t, d, 1.0 / 40320.0); t = fma(t, d, 1.0 / 5040.0);
+  t = fma(t, d, 1.0 / 720.0); t = fma(t, d, 1.0 / 120.0); t = fma(t, d, 1.0 / 24.0); t = fma(t, d, 1.0 / 6.0); t = fma(t, d, 0.5);
+  const double k = d * d * t;
   *up = k + d;
   return k;
 }
-// Loss of a row and its derivative by the row's log-probability.  One lane does this while the others wait, so it takes the
-// exponential of fp32; what is compared with a border is the logarithm, in 64 bits.
+// Loss of a row and its derivative by the row's log-probability; what is compared with a border is the ratio's logarithm.
 __device__ __forceinline__ double policy_row(const PolicyArgs& a, const Rows& of, int row, double logp, double* slope) {
   const double adv = a.advantage[row], x = logp - (double)a.old_logp[row], rho = exp_near(x), w = of.weight_of(row);
   const bool above = x > a.log_hi, below = x < a.log_lo;
@@ -234,7 +258,8 @@ __device__ __forceinline__ void put_no_row(const RowOut& o, int row) {
 template <typename T, int THREADS, int NV, bool NT>
 __device__ __forceinline__ double policy_in_registers(const T* logits, long stride, Rows of, RowOut out, PolicyArgs pol, T* dlogits, long dstride) {
   constexpr int VE = Span<T>::VE, N = THREADS / 64;
-  __shared__ float red_m[N], red_s[N], coef_of;
+  __shared__ double red_s[N];
+  __shared__ float red_m[N], coef_of;
   const int row = blockIdx.x, lane = threadIdx.x;
   T* d = dlogits + (long)row * dstride;
   if (!of.counts(row)) {
@@ -265,18 +290,18 @@ __device__ __forceinline__ double policy_in_registers(const T* logits, long stri
   }
   m = block_max<N>(m, red_m);
   as_loaded(r);
-  float s0 = exp_of(xe, m), s1 = 0.f;  // (a NaN, an infinity and a row of nothing but -infinity make the sum NaN)
+  double acc = (double)exp_for_sum(xe, m);  // (a NaN, an infinity and a row of nothing but -infinity make the sum NaN)
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     float x[VE];
     unpack<T>(r[i], x);
-#pragma unroll
-    for (int e = 0; e < VE; e += 2) { s0 += exp_of(x[e], m); s1 += exp_of(x[e + 1], m); }
+    acc += exp_sum<VE>(x, m);
   }
-  const float s = block_sum<N>(s0 + s1, red_s);
+  const double s64 = block_sum<N>(acc, red_s);
+  const float s = (float)s64;
   double loss = 0.0;
   if (lane == 0) {
-    const double l = log_of(s), lp = ((double)zy - (double)m) - l;
+    const double l = log_of(s64), lp = ((double)zy - (double)m) - l;
     double slope;
     loss = policy_row(pol, of, row, lp, &slope);
     put_row(out, row, lp, (double)m + l, m, s);
@@ -324,7 +349,8 @@ __global__ __launch_bounds__(THREADS, WAVES) void policy_row_kernel(const T* log
 template <typename T, int THREADS, int U, bool POLICY, bool NT>
 __device__ __forceinline__ double row_in_passes(const T* logits, long stride, Rows of, RowOut out, PolicyArgs pol, T* dlogits, long dstride) {
   constexpr int VE = Span<T>::VE, N = THREADS / 64;
-  __shared__ float red_m[N], red_s[N], coef_of;
+  __shared__ double red_s[N];
+  __shared__ float red_m[N], coef_of;
   const int row = blockIdx.x, lane = threadIdx.x;
   T* d = dlogits + (long)row * dstride;
   if (!of.counts(row)) {
@@ -337,8 +363,9 @@ __device__ __forceinline__ double row_in_passes(const T* logits, long stride, Ro
   const uint4* v = reinterpret_cast<const uint4*>(z + sp.head);
   const int edge = sp.edge(lane), target = of.targets[row];
   const float xe = edge >= 0 ? to_f32(z[edge]) : -INFINITY, zy = to_f32(z[target]);
-  float mine = xe, part = edge >= 0 ? 1.f : 0.f;  // the lane's sum counts exp(x - mine)
-  if (xe != xe) part = xe;
+  float mine = xe;
+  double part = edge >= 0 ? 1.0 : 0.0;  // the lane's sum counts exp(x - mine)
+  if (xe != xe) part = (double)xe;
   for (int k0 = lane; k0 < sp.full; k0 += U * THREADS) {
     uint4 r[U];
 #pragma unroll
@@ -352,24 +379,29 @@ __device__ __forceinline__ double row_in_passes(const T* logits, long stride, Ro
       for (int e = 0; e < VE; ++e) top = fmaxf(top, x[e]);
     }
     if (top > mine) {
-      part = mine == -INFINITY ? (part != part ? part : 0.f) : part * exp_of(mine, top);
+      part = mine == -INFINITY ? (part != part ? part : 0.0) : part * (double)exp_for_sum(mine, top);
       mine = top;
     }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       float x[VE];
       unpack<T>(r[i], x);
+      if (mine > -INFINITY) {
+        part += exp_sum<VE>(x, mine);
+      } else {  // nothing but -infinity so far, or a NaN
 #pragma unroll
-      for (int e = 0; e < VE; ++e) part += mine == -INFINITY ? (x[e] != x[e] ? x[e] : 0.f) : exp_of(x[e], mine);
+        for (int e = 0; e < VE; ++e) part += x[e] == x[e] ? 0.0 : (double)x[e];
+      }
     }
   }
   const float m = block_max<N>(mine, red_m);
   // lanes without a finite logit add nothing, unless they saw a NaN; a row without one is undefined
-  const float own = mine == -INFINITY && m > -INFINITY ? (part != part ? part : 0.f) : part * exp_of(mine, m);
-  const float s = block_sum<N>(own, red_s);
+  const double own = mine == -INFINITY && m > -INFINITY ? (part != part ? part : 0.0) : part * (double)exp_for_sum(mine, m);
+  const double s64 = block_sum<N>(own, red_s);
+  const float s = (float)s64;
   double loss = 0.0;
   if (lane == 0) {
-    const double l = log_of(s), lp = ((double)zy - (double)m) - l;
+    const double l = log_of(s64), lp = ((double)zy - (double)m) - l;
     if (POLICY) {
       double slope;
       loss = policy_row(pol, of, row, lp, &slope);
