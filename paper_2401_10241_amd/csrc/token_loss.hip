@@ -595,9 +595,11 @@ Workspace carve(void* base, int rows, int pairs) {
 }
 
 // Lines that no cache would hold until they are wanted again: logits of over 64 MB, a quarter of the last cache (the gradient and
-// what comes next want their place in it too).  us with / without: log-probabilities of 4096 x 50432 bf16 69 / 74, policy loss of the same
-// 149 / 161; 64 x 50432, read from the caches, 9.3 / 7.4 and 12.1 / 9.7.
-bool past_caches(const zb_logits* x) { return (size_t)x->rows * x->vocab * (x->dtype == ZB_BF16 ? 2 : 4) > (size_t)64 << 20; }
+// what comes next want their place in it too); where the logits are read again next, of over all of it.  us with / without:
+// log-probabilities of 4096 x 50432 bf16 69 / 74, policy loss of the same 149 / 161; 64 x 50432, read from the caches, 9.3 / 7.4 and 12.1 / 9.7.
+bool past_caches(const zb_logits* x, bool again = false) {
+  return (size_t)x->rows * x->vocab * (x->dtype == ZB_BF16 ? 2 : 4) > (size_t)(again ? 256 : 64) << 20;
+}
 
 #define ZB_NT(call)                                                          \
   do {                                                                       \
@@ -605,14 +607,13 @@ bool past_caches(const zb_logits* x) { return (size_t)x->rows * x->vocab * (x->d
     else { constexpr bool NT = false; call; }                                \
   } while (0)
 
-// last: nothing reads the logits again
-template <typename T> hipError_t launch_logp(const zb_logits* x, const Rows& of, const RowOut& out, bool last, hipStream_t s) {
+template <typename T> hipError_t launch_logp(const zb_logits* x, const Rows& of, const RowOut& out, bool nt, hipStream_t s) {
   const int vectors = x->vocab / Span<T>::VE;
 #define ZB_LOGP(THREADS, U, NT) \
   row_kernel<T, THREADS, U, false, NT><<<x->rows, THREADS, 0, s>>>((const T*)x->logits, x->row_stride, of, out, PolicyArgs{}, (T*)nullptr, 0)
 #define ZB_ROWS(THREADS, U)                                    \
   do {                                                         \
-    if (last && past_caches(x)) ZB_LOGP(THREADS, U, true);     \
+    if (nt) ZB_LOGP(THREADS, U, true);                         \
     else ZB_LOGP(THREADS, U, false);                           \
   } while (0)
   if (vectors <= 512) ZB_ROWS(64, 4);
@@ -623,8 +624,8 @@ template <typename T> hipError_t launch_logp(const zb_logits* x, const Rows& of,
 #undef ZB_LOGP
   return hipGetLastError();
 }
-hipError_t launch_logp(const zb_logits* x, const Rows& of, const RowOut& out, bool last, hipStream_t s) {
-  return x->dtype == ZB_BF16 ? launch_logp<bf16_t>(x, of, out, last, s) : launch_logp<float>(x, of, out, last, s);
+hipError_t launch_logp(const zb_logits* x, const Rows& of, const RowOut& out, bool nt, hipStream_t s) {
+  return x->dtype == ZB_BF16 ? launch_logp<bf16_t>(x, of, out, nt, s) : launch_logp<float>(x, of, out, nt, s);
 }
 
 template <typename T>
@@ -711,7 +712,7 @@ zb_status preference_loss(const zb_logits* x, const zb_preference* p, double gra
   if (x->rows) {
     RowOut out{logp};
     out.top = w.top; out.inv = w.inv; out.logp64 = w.logp;
-    if (launch_logp(x, of, out, dlogits == nullptr, s) != hipSuccess) return ZB_EDEVICE;
+    if (launch_logp(x, of, out, !dlogits && past_caches(x), s) != hipSuccess) return ZB_EDEVICE;
   }
   if (p->pairs) {
     const PairArgs a{p->ref_logp, p->beta, p->label_smoothing, p->scale, grad_scale};
@@ -729,12 +730,13 @@ using namespace zb;
 
 extern "C" {
 
+// (a caller that asks for lse is about to have the gradient made of the same logits)
 zb_status zb_token_logprobs(const zb_logits* x, float* logp, float* lse, void* hip_stream) {
   if (!valid_logits(x) || (x->rows && !logp) || misaligned(logp, 4) || misaligned(lse, 4)) return ZB_EINVAL;
   if (x->rows == 0) return ZB_OK;
   OnDeviceOf on((hipStream_t)hip_stream);
   if (!on.ok) return ZB_EDEVICE;
-  return said(launch_logp(x, Rows{x->targets, nullptr, nullptr, 0, x->vocab}, RowOut{logp, lse}, true, (hipStream_t)hip_stream));
+  return said(launch_logp(x, Rows{x->targets, nullptr, nullptr, 0, x->vocab}, RowOut{logp, lse}, past_caches(x, lse != nullptr), (hipStream_t)hip_stream));
 }
 
 zb_status zb_token_logprobs_backward(const zb_logits* x, const float* lse, const float* dlogp, void* dlogits, int64_t dlogits_stride,
