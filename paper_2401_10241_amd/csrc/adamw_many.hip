@@ -433,12 +433,17 @@ template <int THREADS, class F> __device__ __forceinline__ void add_parts(long n
   __shared__ int redf[THREADS / 64];
   double acc = 0.0;
   int bad = 0;
-  for (long i = threadIdx.x; i < n; i += THREADS) {
-    double x;
-    int f;
-    part(i, &x, &f);
-    acc += x;
-    bad |= f;
+  for (long i0 = threadIdx.x; i0 < n; i0 += 8 * THREADS) {  // eight loads on their way at a time
+    double x[8];
+    int f[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      x[k] = 0.0;
+      f[k] = 0;
+      if (i0 + k * THREADS < n) part(i0 + k * THREADS, &x[k], &f[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) { acc += x[k]; bad |= f[k]; }
   }
   acc = wave_sum(acc);
   bad = __any(bad);
@@ -485,11 +490,16 @@ template <bool NT> __global__ __launch_bounds__(kThreads) void norm_many_kernel(
       for (int k = 0; k < kNormVectors; ++k) take(get<NT, f32x4>((const float*)q.grad + i0 + (long)k * kChunk));
     }
   } else {
-    for (int k = 0; k < kNormVectors; ++k) {
-      const long i = i0 + (long)k * kChunk;
-      const int live = live_of(q.n, i);
-      if (!live) break;
-      take(load_grad(q, i, live, live == 4 && (q.flags & kWide)));
+    for (int k0 = 0; k0 < kNormVectors && start + k0 * kChunk < q.n; k0 += 4) {
+      f32x4 g[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const long i = i0 + (long)(k0 + k) * kChunk;
+        const int live = live_of(q.n, i);
+        g[k] = load_grad(q, i, live, live == 4 && (q.flags & kWide));
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) take(g[k]);
     }
   }
   double sum = wave_sum((acc[0] + acc[1]) + (acc[2] + acc[3]));

@@ -182,8 +182,9 @@ __device__ __forceinline__ double policy_row(const PolicyArgs& a, const Rows& of
   const double adv = a.advantage[row], x = logp - (double)a.old_logp[row], rho = exp_near(x), w = of.weight_of(row);
   const bool above = x > a.log_hi, below = x < a.log_lo;
   const double held = above ? a.hi : below ? a.lo : rho;
-  double loss = -fmin(rho * adv, held * adv);
-  double g = (adv > 0 && above) || (adv < 0 && below) ? 0.0 : -adv * rho;
+  // (an advantage of 0 asks for nothing, however far the ratio is)
+  double loss = adv == 0 ? 0.0 : -fmin(rho * adv, held * adv);
+  double g = adv == 0 || (adv > 0 && above) || (adv < 0 && below) ? 0.0 : -adv * rho;
   if (a.kl != 0.0) {
     double up;
     loss += a.kl * exp_above_line((double)a.ref_logp[row] - logp, &up);
@@ -197,7 +198,13 @@ __device__ __forceinline__ double policy_row(const PolicyArgs& a, const Rows& of
 template <int THREADS, class F> __device__ __forceinline__ double sum_of(int n, F&& value) {
   __shared__ double red[THREADS / 64];
   double acc = 0.0;
-  for (int i = threadIdx.x; i < n; i += THREADS) acc += value(i);
+  for (int i0 = threadIdx.x; i0 < n; i0 += 4 * THREADS) {  // four loads on their way at a time
+    double x[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = i0 + k * THREADS < n ? value(i0 + k * THREADS) : 0.0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) acc += x[k];
+  }
   acc = wave_sum(acc);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = acc;
   __syncthreads();
@@ -569,7 +576,7 @@ bool valid_logits(const zb_logits* x) {
 }
 bool valid_dlogits(const zb_logits* x, const void* d, int64_t* stride) {
   if (*stride == 0) *stride = x->row_stride;
-  if (*stride < x->vocab || *stride > (int64_t)1 << 32) return false;
+  if (*stride < x->vocab || *stride > (int64_t)1 << 32 || (d && d == x->logits && *stride != x->row_stride)) return false;
   return !((uintptr_t)d & (x->dtype == ZB_BF16 ? 1 : 3));
 }
 bool misaligned(const void* p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
@@ -579,10 +586,6 @@ struct Workspace {  // a counter; per row a partial loss, the log-probability, w
   double *part, *logp;
   float *top, *inv, *coef;
 };
-size_t scratch_bytes(int rows, int pairs) {
-  const size_t n = (size_t)(rows > pairs ? rows : pairs);
-  return n * sizeof(double) + (size_t)rows * (sizeof(double) + 3 * sizeof(float)) + 256;
-}
 Workspace carve(void* base, int rows, int pairs) {
   Workspace w;
   w.done = (unsigned*)base;
@@ -663,7 +666,10 @@ zb_status said(hipError_t e) { return e == hipSuccess ? ZB_OK : ZB_EDEVICE; }
 
 }  // namespace
 
-size_t loss_workspace_bytes(int rows, int pairs) { return scratch_bytes(rows, pairs); }
+size_t loss_workspace_bytes(int rows, int pairs) {
+  const size_t n = (size_t)(rows > pairs ? rows : pairs);
+  return n * sizeof(double) + (size_t)rows * (sizeof(double) + 3 * sizeof(float)) + 256;
+}
 
 bool valid_policy(const zb_policy* p) {
   return p->clip_low >= 0 && p->clip_low <= 1 && p->clip_high >= 0 && p->kl_coef >= 0 && isfinite(p->clip_high) && isfinite(p->kl_coef) && isfinite(p->scale);
@@ -676,7 +682,7 @@ zb_status policy_loss(const zb_logits* x, const zb_policy* p, double grad_scale,
                       void* workspace, size_t workspace_size, hipStream_t s) {
   if (!valid_logits(x) || !p || !loss || !valid_dlogits(x, dlogits, &dlogits_stride) || !valid_policy(p)) return ZB_EINVAL;
   if (x->rows && (!p->old_logp || !p->advantage || (p->kl_coef != 0 && !p->ref_logp))) return ZB_EINVAL;
-  if (!workspace || misaligned(workspace, 8) || workspace_size < scratch_bytes(x->rows, 0)) return ZB_EINVAL;
+  if (!workspace || misaligned(workspace, 8) || workspace_size < loss_workspace_bytes(x->rows, 0)) return ZB_EINVAL;
   if (misaligned(loss, 4) || misaligned(logp, 4) || misaligned(p->old_logp, 4) || misaligned(p->advantage, 4) || misaligned(p->ref_logp, 4) ||
       misaligned(p->weight, 4))
     return ZB_EINVAL;
@@ -701,7 +707,7 @@ zb_status preference_loss(const zb_logits* x, const zb_preference* p, double gra
                           int64_t dlogits_stride, void* workspace, size_t workspace_size, hipStream_t s) {
   if (!valid_logits(x) || !p || !loss || !valid_dlogits(x, dlogits, &dlogits_stride) || !valid_preference(p)) return ZB_EINVAL;
   if ((p->pairs && !p->offsets) || (x->rows && p->pairs && !p->ref_logp)) return ZB_EINVAL;
-  if (!workspace || misaligned(workspace, 8) || workspace_size < scratch_bytes(x->rows, p->pairs)) return ZB_EINVAL;
+  if (!workspace || misaligned(workspace, 8) || workspace_size < loss_workspace_bytes(x->rows, p->pairs)) return ZB_EINVAL;
   if (misaligned(loss, 4) || misaligned(logp, 4) || misaligned(rewards, 4) || misaligned(p->offsets, 4) || misaligned(p->ref_logp, 4) ||
       misaligned(p->weight, 4))
     return ZB_EINVAL;

@@ -345,6 +345,17 @@ def test_large_ratios_and_far_references():
     assert host(loss)[0] == np.inf and not g[0].any() and np.abs(g[1]).max() < 1e-38 and g[2, k.targets[2]] == np.inf
 
 
+def test_an_advantage_of_zero_asks_for_nothing():
+    import torch
+    import paper_2401_10241_amd as zb
+    k = Case("bf16", 3, 70)
+    keep = dev(np.array([-np.inf, -1e30, -3.0], np.float32)), dev(np.zeros(3, np.float32))
+    loss, ws = torch.full((1,), GUARD, device="cuda"), scratch(3)
+    zb.policy_loss(k.x(), zb.policy(keep[0].data_ptr(), keep[1].data_ptr()), loss.data_ptr(), 0, k.dflat.data_ptr(), workspace=ws.data_ptr(),
+                   workspace_bytes=ws.numel())
+    assert host(loss)[0] == 0 and not k.gradient().any()
+
+
 def test_targets_that_the_policy_or_the_reference_rules_out():
     """log-probabilities of -infinity: the ratio is 0, the KL term infinite where the reference allows the token, and no NaN beside them."""
     import torch

@@ -51,6 +51,7 @@ def test_bad_arguments_of_the_logprobs():
         assert rc_of(zb.token_logprobs_backward, x, *a) == zb.EINVAL
     assert rc_of(zb.token_logprobs_backward, x, AT, AT, AT, 99) == zb.EINVAL
     assert rc_of(zb.token_logprobs_backward, x, AT, AT, AT, -104) == zb.EINVAL
+    assert rc_of(zb.token_logprobs_backward, x, AT, AT, AT, 108) == zb.EINVAL  # in place, with another stride
     assert zb.lib.zb_token_logprobs(None, AT, AT, None) == zb.EINVAL
 
 
