@@ -177,9 +177,16 @@ __device__ __forceinline__ double exp_above_line(double d, double* up) {
   *up = k + d;
   return k;
 }
+// What a row's loss reads.
+struct PolicyTerms {
+  float advantage, old_logp, ref_logp, weight;
+};
+__device__ __forceinline__ PolicyTerms terms_of(const PolicyArgs& a, const Rows& of, int row) {
+  return {a.advantage[row], a.old_logp[row], a.kl != 0.0 ? a.ref_logp[row] : 0.f, of.weight ? of.weight[row] : 1.f};
+}
 // Loss of a row and its derivative by the row's log-probability; what is compared with a border is the ratio's logarithm.
-__device__ __forceinline__ double policy_row(const PolicyArgs& a, const Rows& of, int row, double logp, double* slope) {
-  const double adv = a.advantage[row], x = logp - (double)a.old_logp[row], rho = exp_near(x), w = of.weight_of(row);
+__device__ __forceinline__ double policy_row(const PolicyArgs& a, const PolicyTerms& in, double logp, double* slope) {
+  const double adv = in.advantage, x = logp - (double)in.old_logp, rho = exp_near(x), w = in.weight;
   const bool above = x > a.log_hi, below = x < a.log_lo;
   const double held = above ? a.hi : below ? a.lo : rho;
   // (an advantage of 0 asks for nothing, however far the ratio is)
@@ -187,7 +194,7 @@ __device__ __forceinline__ double policy_row(const PolicyArgs& a, const Rows& of
   double g = adv == 0 || (adv > 0 && above) || (adv < 0 && below) ? 0.0 : -adv * rho;
   if (a.kl != 0.0) {
     double up;
-    loss += a.kl * exp_above_line((double)a.ref_logp[row] - logp, &up);
+    loss += a.kl * exp_above_line((double)in.ref_logp - logp, &up);
     g -= a.kl * up;
   }
   *slope = a.grad_scale * w * g;
@@ -267,6 +274,7 @@ __device__ __forceinline__ double policy_in_registers(const T* logits, long stri
   constexpr int VE = Span<T>::VE, N = THREADS / 64;
   __shared__ double red_s[N];
   __shared__ float red_m[N], coef_of;
+  __shared__ PolicyTerms in;
   const int row = blockIdx.x, lane = threadIdx.x;
   T* d = dlogits + (long)row * dstride;
   if (!of.counts(row)) {
@@ -287,6 +295,7 @@ __device__ __forceinline__ double policy_in_registers(const T* logits, long stri
   const float xe = edge >= 0 ? to_f32(z[edge]) : -INFINITY;
   const int target = of.targets[row];
   const float zy = to_f32(z[target]);
+  if (lane == 0) in = terms_of(pol, of, row);  // (on their way with the row; kept apart from it, whose lanes have no registers to spare)
   float m = xe;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -310,7 +319,7 @@ __device__ __forceinline__ double policy_in_registers(const T* logits, long stri
   if (lane == 0) {
     const double l = log_of(s64), lp = ((double)zy - (double)m) - l;
     double slope;
-    loss = policy_row(pol, of, row, lp, &slope);
+    loss = policy_row(pol, in, lp, &slope);
     put_row(out, row, lp, (double)m + l, m, s);
     coef_of = (float)slope;
   }
@@ -411,7 +420,7 @@ __device__ __forceinline__ double row_in_passes(const T* logits, long stride, Ro
     const double l = log_of(s64), lp = ((double)zy - (double)m) - l;
     if (POLICY) {
       double slope;
-      loss = policy_row(pol, of, row, lp, &slope);
+      loss = policy_row(pol, terms_of(pol, of, row), lp, &slope);
       coef_of = (float)slope;
     }
     put_row(out, row, lp, (double)m + l, m, s);
