@@ -19,7 +19,7 @@ namespace zb {
 
 namespace {
 
-constexpr int kThreads = 256, kPerThread = 4, kChunk = kThreads * kPerThread;  // values of a workgroup that only moves them
+constexpr int kThreads = 256, kPerThread = 4, kChunk = kThreads * kPerThread;  // values of a workgroup
 constexpr int kBlock = 256;                                                   // values that share scales
 static_assert(kBlock == kWave * kPerThread, "a wave holds one block");
 
@@ -257,8 +257,7 @@ __device__ __forceinline__ float block_top(float v) {
   return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63));
 }
 
-// The step of four values of a lane from value i on, in two parts so that the loads of the next four can be on their way before the
-// first are worked on; WHOLE: all lanes have four, aligned.
+// The step of four values of a lane from value i on; WHOLE: all lanes have four, aligned.
 template <bool BITS8, bool WHOLE, bool NT> struct Four {
   long i;
   int live;
@@ -351,31 +350,29 @@ template <bool BITS8, bool WHOLE, bool NT> struct Four {
   }
 };
 
-constexpr int kRounds8 = 1, kRounds32 = 1;
+// One workgroup per 1024 values; which tensor they belong to stands in the launch's arguments.  32 bits: bound by HBM, 315M values with bf16
+// gradients and copies 1460 us = 6.0 TB/s (a large copy moves 4.9, a kernel that changes an array in place 5.9).  8 bits: the same 990 to 1055 us,
+// 5.1 to 4.8 TB/s, about 105 instructions a value, half of them for the codes, which the memory's 800 us do not hide all of.
+// (Two chunks a workgroup, the second's loads on their way before the first is worked on: 1057 us where one took 1044; eight values of a lane
+// instead of four: 96 registers and 1530 us.)
 template <bool BITS8, bool NT>
 __global__ __launch_bounds__(kThreads) void adamw_many_kernel(Table tab, Hyper hp, const Clock* __restrict__ clk_at) {
-  constexpr int ROUNDS = BITS8 ? kRounds8 : kRounds32;
   const Clock clk = *clk_at;
   if (!clk.go) return;
   const Tensor& q = tensor_of(tab, blockIdx.x);
-  const long at = (long)(blockIdx.x - q.wg0) * (kChunk * ROUNDS), i = at + threadIdx.x * kPerThread;
-  if (q.n - at >= kChunk * ROUNDS && (q.flags & kWide)) {
-    Four<BITS8, true, NT> f[ROUNDS];
-#pragma unroll
-    for (int k = 0; k < ROUNDS; ++k) f[k].load(q, i + k * kChunk);
-#pragma unroll
-    for (int k = 0; k < ROUNDS; ++k) f[k].finish(q, hp, clk);
+  const long at = (long)(blockIdx.x - q.wg0) * kChunk, i = at + threadIdx.x * kPerThread;
+  if (q.n - at >= kChunk && (q.flags & kWide)) {
+    Four<BITS8, true, NT> f;
+    f.load(q, i);
+    f.finish(q, hp, clk);
   } else {
-#pragma unroll 1
-    for (int k = 0; k < ROUNDS && at + k * kChunk < q.n; ++k) {
-      Four<BITS8, false, NT> f;
-      f.load(q, i + k * kChunk);
-      f.finish(q, hp, clk);
-    }
+    Four<BITS8, false, NT> f;
+    f.load(q, i);
+    f.finish(q, hp, clk);
   }
 }
 
-// moments held in 8 bits as values: Tensor.theta is where m's go, Tensor.grad v's
+// Moments held in 8 bits as values (bound by HBM: 315M values 500 us = 6.3 TB/s): Tensor.theta is where m's go, Tensor.grad v's
 __global__ __launch_bounds__(kThreads) void read_moments_kernel(Table tab) {
   const Tensor& q = tensor_of(tab, blockIdx.x);
   const long i = (long)(blockIdx.x - q.wg0) * kChunk + threadIdx.x * kPerThread;
@@ -458,7 +455,8 @@ __global__ __launch_bounds__(1024) void norm_sum_kernel(const double* __restrict
                                                         double* __restrict__ sq_out, int* __restrict__ nf_out) {
   add_parts<1024>(parts, [&](long i, double* x, int* f) { *x = part_sq[i]; *f = part_nf[i]; }, sq_out, nf_out);
 }
-// One part per workgroup.  A launch of up to kNormInPlace of them adds the parts itself: the workgroup that is through last does, reading past
+// One part per workgroup; bound by HBM: 315M bf16 gradients 96 us = 6.6 TB/s (chunks of 4 / 8 / 16 / 32 times 1024 values: 123 / 105 / 102 /
+// 100).  A launch of up to kNormInPlace of them adds the parts itself: the workgroup that is through last does, reading past
 // the caches of the XCDs what the others wrote past them; `done` counts modulo the workgroups, so it is 0 again for the next call.
 template <bool NT> __global__ __launch_bounds__(kThreads) void norm_many_kernel(Table tab, double* part_sq, int* part_nf, NormOut out) {
   __shared__ double red[kThreads / 64];
@@ -657,12 +655,12 @@ zb_status zb_adamw_step(const zb_adamw_config* cfg, const zb_adamw_tensor* tenso
   if (hipGetLastError() != hipSuccess) return ZB_EDEVICE;
   const bool b8 = cfg->bits == 8;
   // States that no cache would hold until the next step: more than the 256 MB of the last one.  us of 315M values with bf16 gradients with /
-  // without: 32 bits 1461 / 1639, 8 bits 1114 / 1132.
+  // without the caches' being told: 32 bits 1461 / 1639, 8 bits 1114 / 1132.
   double held = 0.0;
   for (int32_t k = 0; k < count; ++k) held += (double)tensors[k].n * (b8 ? 6 : 12);
   const bool nt = held > 256.0 * (1 << 20);
   const hipError_t e = for_tables(
-      tensors, count, kChunk * (b8 ? kRounds8 : kRounds32),
+      tensors, count, kChunk,
       [&](int32_t k, Tensor* q) {
         const zb_adamw_tensor& t = tensors[k];
         q->theta = t.theta; q->grad = t.grad; q->copy16 = (bf16_t*)t.copy16; q->m = t.m; q->v = t.v; q->m_scale = t.m_scale; q->v_scale = t.v_scale;

@@ -268,7 +268,9 @@ __device__ __forceinline__ void put_no_row(const RowOut& o, int row) {
 }
 
 // The policy loss, one workgroup per row, the row in registers (NV vectors a lane): read once for the maximum, the sum and the
-// gradient, which follows from the row's own log-probability.
+// gradient, which follows from the row's own log-probability.  Bound by HBM: 4096 rows of 50432 bf16, 800 of them without weight, 141 us =
+// 5.3 TB/s of what has to move (a large copy moves 4.9); 1023 rows of 32003 fp32 51 us.  While one lane works out the row's
+// coefficient nothing of that row moves, so a CU holds two rows of 100 KB (64 registers a lane): one of them at a time takes 209 us.
 template <typename T, int THREADS, int NV, bool NT>
 __device__ __forceinline__ double policy_in_registers(const T* logits, long stride, Rows of, RowOut out, PolicyArgs pol, T* dlogits, long dstride) {
   constexpr int VE = Span<T>::VE, N = THREADS / 64;
@@ -360,8 +362,9 @@ __global__ __launch_bounds__(THREADS, WAVES) void policy_row_kernel(const T* log
   add_to_total<THREADS>(out.total, out.part, policy_in_registers<T, THREADS, NV, NT>(logits, stride, of, out, pol, dlogits, dstride));
 }
 
-// lse and log-probability, one workgroup per row: maximum and sum in one pass, U vectors of a lane at a time.  With POLICY, for rows that
-// registers do not hold, the policy loss: the row is read again for the gradient.
+// lse and log-probability, one workgroup per row: maximum and sum in one pass, U vectors of a lane at a time, the sum scaled anew when the lane's
+// maximum grows.  Bound by HBM: 4096 rows of 50432 bf16 65 us = 6.4 TB/s (with the row in registers 82).  With POLICY, for
+// rows that registers do not hold, the policy loss: the row is read again for the gradient (1536 rows of 131072 bf16 185 us).
 template <typename T, int THREADS, int U, bool POLICY, bool NT>
 __device__ __forceinline__ double row_in_passes(const T* logits, long stride, Rows of, RowOut out, PolicyArgs pol, T* dlogits, long dstride) {
   constexpr int VE = Span<T>::VE, N = THREADS / 64;
@@ -457,9 +460,10 @@ __global__ __launch_bounds__(THREADS) void row_kernel(const T* logits, long stri
   if (POLICY) add_to_total<THREADS>(out.total, out.part, loss);
 }
 
-// coef ([j = target] - exp(z_j - top) inv), inv null: 1, by workgroups of kThreads * kGradVectors vectors of a row (us of 5513 rows
-// of 50432 bf16 after their log-probabilities with 2 / 4 / 8 vectors a lane: 236 / 239 / 258; from the last row to the first, towards what the
-// caches may still hold: 239)
+// coef ([j = target] - exp(z_j - top) inv), inv null: 1, by workgroups of kThreads * kGradVectors vectors of a row.  Bound by HBM: the rows of
+// six pairs of about 500 tokens x 50432 bf16, which have just been read for their log-probabilities, 144 us = 6.8 TB/s with the
+// rows without weight, which are not read.  us of log-probabilities and gradient with 2 / 4 / 8 vectors a lane: 229 / 239 / 258; from the
+// last row to the first, towards what the caches may still hold: 239.
 constexpr int kGradVectors = 2;
 template <typename T, bool NT>
 __global__ __launch_bounds__(kThreads) void grad_kernel(const T* logits, long stride, Rows of, const float* __restrict__ coefs,
@@ -537,7 +541,8 @@ __device__ __forceinline__ void sequence_rows(const int* offsets, int q, int row
   *b = y < *a ? *a : y > rows ? rows : y;
 }
 
-// One workgroup per pair: both sequences' sums of w (logp - ref), the pair's loss, and the coefficient of every row.
+// One workgroup per pair: both sequences' sums of w (logp - ref), the pair's loss, and the coefficient of every row.  A chain of loads, sums
+// and one lane's exponential: 5.7 us for two pairs of 50 tokens, 8.7 for six of 500.
 constexpr int kPairThreads = 1024;
 __global__ __launch_bounds__(kPairThreads) void pair_kernel(PairArgs a, Rows of, int rows, const double* __restrict__ logp, float* __restrict__ rewards,
                                                             float* __restrict__ coef, double* part, Total total) {
@@ -628,6 +633,9 @@ template <typename T> hipError_t launch_logp(const zb_logits* x, const Rows& of,
     if (nt) ZB_LOGP(THREADS, U, true);                         \
     else ZB_LOGP(THREADS, U, false);                           \
   } while (0)
+  // Lanes of a workgroup by the length of a row, us of 8192 rows of 2048 / 8192 bf16 and 4096 of 32000 / 50432: 64 lanes 8.8 / - / - / -, 256
+  // 12.0 / 22.0 / 44.8 / 72.6, 512 - / 36.0 / 42.3 / 69.0, 1024 - / - / 47.2 / 73.4; 64 rows of 50432, where most of the chip is idle: 512 lanes 7.4,
+  // 1024 6.4.
   if (vectors <= 512) ZB_ROWS(64, 4);
   else if (vectors <= 2048) ZB_ROWS(256, 4);
   else if (x->rows >= 512) ZB_ROWS(512, 4);
@@ -643,6 +651,9 @@ hipError_t launch_logp(const zb_logits* x, const Rows& of, const RowOut& out, bo
 template <typename T>
 hipError_t launch_policy(const zb_logits* x, const Rows& of, const RowOut& out, const PolicyArgs& pol, void* dlogits, int64_t dstride, hipStream_t s) {
   const int vectors = x->vocab / Span<T>::VE;  // at most: a row's start may leave one fewer
+  // The fewest lanes that hold a row and leave room for a second one on the CU; WAVES per SIMD keep the registers to that.  us of 4096 rows of 32000
+  // bf16: 256 lanes 117, 512 100, 1024 105; of 50432: 256 200, 512 176, 1024 162 (with the caches' part); 2048 rows of 32000 fp32: 512 lanes
+  // 99, 1024 103, in passes 110; of 50432 fp32: 512 lanes 158 (up to 19 registers in memory), in passes 181.
 #define ZB_ROWS(THREADS, NV, WAVES)                                                                                                              \
   if (vectors <= THREADS * NV) {                                                                                                                 \
     ZB_NT((policy_row_kernel<T, THREADS, NV, WAVES, NT><<<x->rows, THREADS, 0, s>>>((const T*)x->logits, x->row_stride, of, out, pol, (T*)dlogits, \
