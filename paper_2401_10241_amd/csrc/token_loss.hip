@@ -231,18 +231,21 @@ struct Total {
   float* loss;     // null: a kernel of its own adds the partial losses
   unsigned* done;
 };
-template <int THREADS> __device__ __forceinline__ void add_to_total(const Total& t, double* part, double mine) {  // mine: lane 0's
-  __shared__ bool last;
+// By one lane, once in a workgroup; *last tells whether all the others have been here.  It comes before a row's gradient is written: the count
+// waits until what its XCD has written is past the caches.
+__device__ __forceinline__ void announce(const Total& t, double* part, double mine, bool* last) {
+  *last = false;
   if (!t.loss) {
-    if (threadIdx.x == 0) part[blockIdx.x] = mine;
+    part[blockIdx.x] = mine;
     return;
   }
-  if (threadIdx.x == 0) {
-    __hip_atomic_store(part + blockIdx.x, mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    last = __builtin_amdgcn_atomic_inc32(t.done, gridDim.x - 1, __ATOMIC_ACQ_REL, "agent") == gridDim.x - 1;
-  }
+  __hip_atomic_store(part + blockIdx.x, mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  *last = __builtin_amdgcn_atomic_inc32(t.done, gridDim.x - 1, __ATOMIC_ACQ_REL, "agent") == gridDim.x - 1;
+}
+template <int THREADS> __device__ __forceinline__ void add_up(const Total& t, const double* part, const bool* last) {  // by the whole workgroup
+  if (!t.loss) return;
   __syncthreads();
-  if (!last) return;
+  if (!*last) return;
   const double s = sum_of<THREADS>((int)gridDim.x, [&](int i) { return __hip_atomic_load(part + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); });
   if (threadIdx.x == 0) *t.loss = (float)s;
 }
@@ -272,7 +275,8 @@ __device__ __forceinline__ void put_no_row(const RowOut& o, int row) {
 // 5.3 TB/s of what has to move (a large copy moves 4.9); 1023 rows of 32003 fp32 51 us.  While one lane works out the row's
 // coefficient nothing of that row moves, so a CU holds two rows of 100 KB (64 registers a lane): one of them at a time takes 209 us.
 template <typename T, int THREADS, int NV, bool NT>
-__device__ __forceinline__ double policy_in_registers(const T* logits, long stride, Rows of, RowOut out, PolicyArgs pol, T* dlogits, long dstride) {
+__device__ __forceinline__ void policy_in_registers(const T* logits, long stride, Rows of, RowOut out, PolicyArgs pol, T* dlogits, long dstride,
+                                                    bool* last) {
   constexpr int VE = Span<T>::VE, N = THREADS / 64;
   __shared__ double red_s[N];
   __shared__ float red_m[N], coef_of;
@@ -280,9 +284,12 @@ __device__ __forceinline__ double policy_in_registers(const T* logits, long stri
   const int row = blockIdx.x, lane = threadIdx.x;
   T* d = dlogits + (long)row * dstride;
   if (!of.counts(row)) {
-    if (lane == 0) put_no_row(out, row);
+    if (lane == 0) {
+      put_no_row(out, row);
+      announce(out.total, out.part, 0.0, last);
+    }
     if (dlogits) clear_row<T, NT>(d, of.vocab, THREADS);
-    return 0.0;
+    return;
   }
   const T* z = logits + (long)row * stride;
   const Span<T> sp(z, of.vocab);
@@ -325,12 +332,13 @@ __device__ __forceinline__ double policy_in_registers(const T* logits, long stri
     put_row(out, row, lp, (double)m + l, m, s);
     coef_of = (float)slope;
   }
-  if (!dlogits) return loss;
-  __syncthreads();
+  if (dlogits) __syncthreads();
+  if (lane == 0) announce(out.total, out.part, loss, last);
+  if (!dlogits) return;
   const float coef = coef_of, neg = -coef / s;
   if (coef == 0.f) {
     clear_row<T, NT>(d, of.vocab, THREADS);
-    return loss;
+    return;
   }
   const bool same = (((uintptr_t)d ^ (uintptr_t)z) & 15) == 0;
   as_loaded(r);
@@ -354,28 +362,32 @@ __device__ __forceinline__ double policy_in_registers(const T* logits, long stri
   // the lane that wrote the target's entry writes it again, whole
   const int kt = target - sp.head;
   if (kt >= 0 && kt < sp.full * VE ? (kt / VE) % THREADS == lane : edge == target) d[target] = from_f32<T>(coef * (1.f - exp_of(zy, m) / s));
-  return loss;
 }
 template <typename T, int THREADS, int NV, int WAVES, bool NT>
 __global__ __launch_bounds__(THREADS, WAVES) void policy_row_kernel(const T* logits, long stride, Rows of, RowOut out, PolicyArgs pol, T* dlogits,
                                                                     long dstride) {
-  add_to_total<THREADS>(out.total, out.part, policy_in_registers<T, THREADS, NV, NT>(logits, stride, of, out, pol, dlogits, dstride));
+  __shared__ bool last;
+  policy_in_registers<T, THREADS, NV, NT>(logits, stride, of, out, pol, dlogits, dstride, &last);
+  add_up<THREADS>(out.total, out.part, &last);
 }
 
 // lse and log-probability, one workgroup per row: maximum and sum in one pass, U vectors of a lane at a time, the sum scaled anew when the lane's
 // maximum grows.  Bound by HBM: 4096 rows of 50432 bf16 65 us = 6.4 TB/s (with the row in registers 82).  With POLICY, for
 // rows that registers do not hold, the policy loss: the row is read again for the gradient (1536 rows of 131072 bf16 185 us).
 template <typename T, int THREADS, int U, bool POLICY, bool NT>
-__device__ __forceinline__ double row_in_passes(const T* logits, long stride, Rows of, RowOut out, PolicyArgs pol, T* dlogits, long dstride) {
+__device__ __forceinline__ void row_in_passes(const T* logits, long stride, Rows of, RowOut out, PolicyArgs pol, T* dlogits, long dstride, bool* last) {
   constexpr int VE = Span<T>::VE, N = THREADS / 64;
   __shared__ double red_s[N];
   __shared__ float red_m[N], coef_of;
   const int row = blockIdx.x, lane = threadIdx.x;
   T* d = dlogits + (long)row * dstride;
   if (!of.counts(row)) {
-    if (lane == 0) put_no_row(out, row);
+    if (lane == 0) {
+      put_no_row(out, row);
+      if (POLICY) announce(out.total, out.part, 0.0, last);
+    }
     if (POLICY && dlogits) clear_row<T, NT>(d, of.vocab, THREADS);
-    return 0.0;
+    return;
   }
   const T* z = logits + (long)row * stride;
   const Span<T> sp(z, of.vocab);
@@ -428,12 +440,14 @@ __device__ __forceinline__ double row_in_passes(const T* logits, long stride, Ro
     }
     put_row(out, row, lp, (double)m + l, m, s);
   }
-  if (!POLICY || !dlogits) return loss;
-  __syncthreads();
+  if (!POLICY) return;
+  if (dlogits) __syncthreads();
+  if (lane == 0) announce(out.total, out.part, loss, last);
+  if (!dlogits) return;
   const float coef = coef_of, neg = -coef / s;
   if (coef == 0.f) {
     clear_row<T, NT>(d, of.vocab, THREADS);
-    return loss;
+    return;
   }
   const bool same = (((uintptr_t)d ^ (uintptr_t)z) & 15) == 0;
   for (int k = lane; k < sp.full; k += THREADS) {  // (a lane reads its entries before it writes them: d may be z)
@@ -452,12 +466,12 @@ __device__ __forceinline__ double row_in_passes(const T* logits, long stride, Ro
   if (edge >= 0) d[edge] = from_f32<T>(neg * exp_of(xe, m));
   const int kt = target - sp.head;
   if (kt >= 0 && kt < sp.full * VE ? (kt / VE) % THREADS == lane : edge == target) d[target] = from_f32<T>(coef * (1.f - exp_of(zy, m) / s));
-  return loss;
 }
 template <typename T, int THREADS, int U, bool POLICY, bool NT>
 __global__ __launch_bounds__(THREADS) void row_kernel(const T* logits, long stride, Rows of, RowOut out, PolicyArgs pol, T* dlogits, long dstride) {
-  const double loss = row_in_passes<T, THREADS, U, POLICY, NT>(logits, stride, of, out, pol, dlogits, dstride);
-  if (POLICY) add_to_total<THREADS>(out.total, out.part, loss);
+  __shared__ bool last;
+  row_in_passes<T, THREADS, U, POLICY, NT>(logits, stride, of, out, pol, dlogits, dstride, &last);
+  if (POLICY) add_up<THREADS>(out.total, out.part, &last);
 }
 
 // coef ([j = target] - exp(z_j - top) inv), inv null: 1, by workgroups of kThreads * kGradVectors vectors of a row.  Bound by HBM: the rows of
@@ -547,6 +561,7 @@ constexpr int kPairThreads = 1024;
 __global__ __launch_bounds__(kPairThreads) void pair_kernel(PairArgs a, Rows of, int rows, const double* __restrict__ logp, float* __restrict__ rewards,
                                                             float* __restrict__ coef, double* part, Total total) {
   __shared__ double red[2][kPairThreads / 64], slope_of;
+  __shared__ bool last;
   int lo[2], hi[2];
   for (int q = 0; q < 2; ++q) {
     sequence_rows(of.offsets, 2 * blockIdx.x + q, rows, &lo[q], &hi[q]);
@@ -574,10 +589,11 @@ __global__ __launch_bounds__(kPairThreads) void pair_kernel(PairArgs a, Rows of,
     slope_of = a.grad_scale * a.beta * (a.smoothing * above - (1.0 - a.smoothing) * below);
   }
   __syncthreads();
+  if (threadIdx.x == 0) announce(total, part, loss, &last);
   const double slope = slope_of;
   for (int q = 0; q < 2; ++q)
     for (int r = lo[q] + threadIdx.x; r < hi[q]; r += kPairThreads) coef[r] = (float)((q ? -slope : slope) * of.weight_of(r));
-  add_to_total<kPairThreads>(total, part, loss);
+  add_up<kPairThreads>(total, part, &last);
 }
 
 constexpr int kMaxRows = 1 << 24;
