@@ -359,8 +359,9 @@ typedef struct {
 zb_status zb_token_logprobs(const zb_logits* x, float* logp, float* lse, void* hip_stream);
 
 /* dlogits[r, j] = dlogp[r] * ([j == targets[r]] - exp(logits[r, j] - lse[r])), with zb_token_logprobs' lse.  A row
- * whose dlogp is 0 is not read and gets zeros.  dlogits may be the logits themselves (then with the same stride, ZB_EINVAL
- * otherwise) and must not overlap them in any other way; dlogits_stride 0 stands for x->row_stride.  Only [rows, vocab] is written. */
+ * whose dlogp is 0 is not read and gets zeros.  dlogits may be the logits themselves (then with the same stride,
+ * ZB_EINVAL otherwise) and must not overlap them in any other way; dlogits_stride 0 stands for x->row_stride.  Only
+ * [rows, vocab] is written. */
 zb_status zb_token_logprobs_backward(const zb_logits* x, const float* lse, const float* dlogp, void* dlogits,
                                      int64_t dlogits_stride, void* hip_stream);
 
@@ -372,8 +373,8 @@ zb_status zb_loss_workspace_bytes(int32_t rows, int32_t pairs, size_t* bytes);
  *   loss = scale * sum over the rows of weight * (-min(rho A, clip(rho, 1 - clip_low, 1 + clip_high) A)
  *                                                 + kl_coef * (exp(d) - d - 1)),   A = advantage,
  * and its gradient with respect to the logits (old_logp, ref_logp and A are constants).  Where the clipped term is
- * the smaller one it passes no gradient; an advantage of 0 gives neither loss nor gradient, whatever rho is.  A row of weight 0 does not count (as above: nothing of it is read, its old_logp,
- * ref_logp and advantage included). */
+ * the smaller one it passes no gradient; an advantage of 0 gives neither loss nor gradient, whatever rho is.  A row of
+ * weight 0 does not count (as above; what its old_logp, ref_logp and advantage hold does not matter). */
 typedef struct {
   const float *old_logp, *advantage; /* device, [rows] */
   const float* ref_logp;             /* device, [rows]; may be NULL if kl_coef is 0 */
@@ -388,7 +389,7 @@ zb_status zb_policy_loss(const zb_logits* x, const zb_policy* p, float* loss, fl
 /* Preference loss of pairs of sequences, the preferred one first: sequence q holds rows offsets[q] .. offsets[q + 1] - 1 (none
  * is allowed), S_q = the sum over its rows of weight * (logp - ref_logp), x = beta * (S_2i - S_2i+1),
  *   loss = scale * sum over i of -(1 - label_smoothing) log sigma(x) - label_smoothing log sigma(-x).
- * Rows of weight 0 and rows before the first or behind the last sequence do not count. */
+ * Rows of weight 0 and rows before the first or behind the last sequence do not count, whatever their ref_logp holds. */
 typedef struct {
   const float* ref_logp;   /* device, [rows] */
   const float* weight;     /* device, [rows], or NULL: 1 each */
@@ -434,10 +435,11 @@ zb_status zb_adamw_grad_norm(const zb_adamw_tensor* tensors, int32_t count, doub
                              void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* One step.  state: ZB_ADAMW_STATE_BYTES of device memory, 8-byte aligned, zero before the first step; its first 8 bytes
- * hold the number of steps taken as an int64 (a caller that resumes writes it there), so a state belongs to one list of tensors.  sq and nonfinite (device, both or
- * neither): the squared norm and the flag of all gradients that are clipped together, of this list or of more; the
- * gradients are scaled by min(1, clip / (sqrt(sq) + 1e-6)), and if the flag is set or sq is not finite nothing changes,
- * the number of steps included.  8-bit states need them: they cannot hold a NaN. */
+ * hold the number of steps taken as an int64 (a caller that resumes writes it there), so a state belongs to one list of
+ * tensors.  sq and nonfinite (device, both or neither): the squared norm and the flag of all gradients that are clipped
+ * together, of this list or of more; the gradients are scaled by min(1, clip / (sqrt(sq) + 1e-6)), and if the flag is
+ * set or sq is not finite nothing changes, the number of steps included.  8-bit states need them: they cannot hold a
+ * NaN.  lr is a value of the call: a captured step keeps the one it was captured with. */
 #define ZB_ADAMW_STATE_BYTES 64
 zb_status zb_adamw_step(const zb_adamw_config* cfg, const zb_adamw_tensor* tensors, int32_t count, double lr, void* state,
                         const double* sq, const int32_t* nonfinite, void* hip_stream);
