@@ -351,7 +351,7 @@ typedef struct {
   const void* logits;      /* device */
   const int32_t* targets;  /* device, [rows] */
   int64_t row_stride;      /* elements, <= 2^32 */
-  int32_t rows, vocab;     /* rows <= 2^24, 1 <= vocab <= 2^18 */
+  int32_t rows, vocab;     /* rows < 2^22, 1 <= vocab <= 2^18 */
   int32_t dtype;           /* zb_dtype of logits and gradient */
 } zb_logits;
 
@@ -394,7 +394,7 @@ typedef struct {
   const float* ref_logp;   /* device, [rows] */
   const float* weight;     /* device, [rows], or NULL: 1 each */
   const int32_t* offsets;  /* device, [2 * pairs + 1], not decreasing, in [0, rows] */
-  int32_t pairs;           /* may be 0 */
+  int32_t pairs;           /* 0 <= pairs < 2^22 */
   double beta, label_smoothing, scale; /* 0 <= label_smoothing <= 1 */
 } zb_preference;
 /* rewards: device, [2 * pairs], beta * S_q, or NULL; the others as for zb_policy_loss. */

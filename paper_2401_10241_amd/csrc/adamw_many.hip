@@ -30,7 +30,7 @@ struct Tensor {
   void *m, *v;
   float *m_scale, *v_scale;
   long n, first;
-  unsigned wg0;    // first workgroup of this tensor
+  int wg0;         // first workgroup of this tensor; negative if earlier launches did a part of it
   unsigned flags;  // kGrad16 | kDecay | kWide
 };
 constexpr unsigned kGrad16 = 1, kDecay = 2, kWide = 4;  // kWide: all accesses of four values are aligned
@@ -61,7 +61,7 @@ __device__ __forceinline__ const Tensor& tensor_of(const Table& tab, unsigned wg
   int a = 0, b = tab.count;
   while (b - a > 1) {
     const int mid = (a + b) >> 1;
-    if (tab.t[mid].wg0 <= wg) a = mid; else b = mid;
+    if (tab.t[mid].wg0 <= (int)wg) a = mid; else b = mid;
   }
   return tab.t[a];
 }
@@ -360,7 +360,7 @@ __global__ __launch_bounds__(kThreads) void adamw_many_kernel(Table tab, Hyper h
   const Clock clk = *clk_at;
   if (!clk.go) return;
   const Tensor& q = tensor_of(tab, blockIdx.x);
-  const long at = (long)(blockIdx.x - q.wg0) * kChunk, i = at + threadIdx.x * kPerThread;
+  const long at = (long)((int)blockIdx.x - q.wg0) * kChunk, i = at + threadIdx.x * kPerThread;
   if (q.n - at >= kChunk && (q.flags & kWide)) {
     Four<BITS8, true, NT> f;
     f.load(q, i);
@@ -375,7 +375,7 @@ __global__ __launch_bounds__(kThreads) void adamw_many_kernel(Table tab, Hyper h
 // Moments held in 8 bits as values (bound by HBM: 315M values 500 us = 6.3 TB/s): Tensor.theta is where m's go, Tensor.grad v's
 __global__ __launch_bounds__(kThreads) void read_moments_kernel(Table tab) {
   const Tensor& q = tensor_of(tab, blockIdx.x);
-  const long i = (long)(blockIdx.x - q.wg0) * kChunk + threadIdx.x * kPerThread;
+  const long i = (long)((int)blockIdx.x - q.wg0) * kChunk + threadIdx.x * kPerThread;
   const int live = live_of(q.n, i);
   if (!live) return;
   const bool wide = live == 4 && (q.flags & kWide);
@@ -394,7 +394,7 @@ __global__ __launch_bounds__(kThreads) void read_moments_kernel(Table tab) {
 // values into 8 bits, each to the nearer code
 __global__ __launch_bounds__(kThreads) void write_moments_kernel(Table tab) {
   const Tensor& q = tensor_of(tab, blockIdx.x);
-  const long i = (long)(blockIdx.x - q.wg0) * kChunk + threadIdx.x * kPerThread;
+  const long i = (long)((int)blockIdx.x - q.wg0) * kChunk + threadIdx.x * kPerThread;
   const int live = live_of(q.n, i);
   const bool wide = live == 4 && (q.flags & kWide);
   float tm = 0.f, tv = 0.f;
@@ -463,7 +463,7 @@ template <bool NT> __global__ __launch_bounds__(kThreads) void norm_many_kernel(
   __shared__ int redf[kThreads / 64];
   __shared__ bool last;
   const Tensor& q = tensor_of(tab, blockIdx.x);
-  const long start = (long)(blockIdx.x - q.wg0) * kNormChunk, i0 = start + threadIdx.x * kPerThread;
+  const long start = (long)((int)blockIdx.x - q.wg0) * kNormChunk, i0 = start + threadIdx.x * kPerThread;
   double acc[4] = {0.0, 0.0, 0.0, 0.0};
   int bad = 0;
   auto take = [&](const f32x4& g) {
@@ -541,32 +541,37 @@ bool valid_codes(const zb_adamw_tensor& t) {
   return t.m && t.v && t.m_scale && t.v_scale && !misaligned(t.m_scale, 4) && !misaligned(t.v_scale, 4);
 }
 
-// Walks the tensors in launches of at most kTensors; start(table, workgroups) issues one.  `chunk` values per workgroup,
-// fill(tensor, row of the table) says what the kernel finds there and returns whether its accesses are aligned.
+// Walks the tensors in launches of at most kTensors and kMaxWorkgroups (a launch has less than 2^32 lanes; 2^34 values pass that);
+// start(table, workgroups) issues one.  `chunk` values per workgroup, fill(tensor, row of the table) says what the kernel finds
+// there and returns whether its accesses are aligned.
+constexpr long kMaxWorkgroups = (1L << 32) / kThreads - 1;
 template <class Fill, class Start>
 hipError_t for_tables(const zb_adamw_tensor* t, int32_t count, long chunk, Fill&& fill, Start&& start) {
   Table tab;
   tab.count = 0;
-  unsigned wgs = 0;
+  long wgs = 0;
   for (int32_t k = 0; k < count; ++k) {
-    if (t[k].n == 0) continue;
     const long need = (t[k].n + chunk - 1) / chunk;
-    if (tab.count == kTensors || (tab.count && wgs + need > 0x7FFFFFFF)) {
-      hipError_t e = start(tab, wgs);
-      if (e != hipSuccess) return e;
-      tab.count = 0;
-      wgs = 0;
+    for (long done = 0; done < need;) {
+      if (tab.count == kTensors || wgs == kMaxWorkgroups) {
+        hipError_t e = start(tab, (unsigned)wgs);
+        if (e != hipSuccess) return e;
+        tab.count = 0;
+        wgs = 0;
+      }
+      Tensor& q = tab.t[tab.count++];
+      q = Tensor{};
+      q.n = t[k].n;
+      q.first = t[k].first;
+      q.wg0 = (int)(wgs - done);
+      q.flags = (t[k].grad_dtype == ZB_BF16 ? kGrad16 : 0) | (t[k].decay ? kDecay : 0);
+      if (fill(k, &q)) q.flags |= kWide;
+      const long now = need - done < kMaxWorkgroups - wgs ? need - done : kMaxWorkgroups - wgs;
+      done += now;
+      wgs += now;
     }
-    Tensor& q = tab.t[tab.count++];
-    q = Tensor{};
-    q.n = t[k].n;
-    q.first = t[k].first;
-    q.wg0 = wgs;
-    q.flags = (t[k].grad_dtype == ZB_BF16 ? kGrad16 : 0) | (t[k].decay ? kDecay : 0);
-    if (fill(k, &q)) q.flags |= kWide;
-    wgs += (unsigned)need;
   }
-  return tab.count ? start(tab, wgs) : hipSuccess;
+  return tab.count ? start(tab, (unsigned)wgs) : hipSuccess;
 }
 
 int32_t live_tensors(const zb_adamw_tensor* t, int32_t count) {

@@ -482,9 +482,9 @@ constexpr int kGradVectors = 2;
 template <typename T, bool NT>
 __global__ __launch_bounds__(kThreads) void grad_kernel(const T* logits, long stride, Rows of, const float* __restrict__ coefs,
                                                         const float* __restrict__ tops, const float* __restrict__ invs, T* dlogits, long dstride,
-                                                        int parts) {
+                                                        int parts, int row0) {
   constexpr int VE = Span<T>::VE;
-  const int row = blockIdx.x / parts, part = blockIdx.x - row * parts, lane = threadIdx.x;
+  const int at_row = blockIdx.x / parts, part = blockIdx.x - at_row * parts, row = row0 + at_row, lane = threadIdx.x;
   const float coef = of.counts(row) ? coefs[row] : 0.f;
   const T* z = logits + (long)row * stride;
   T* d = dlogits + (long)row * dstride;
@@ -596,7 +596,7 @@ __global__ __launch_bounds__(kPairThreads) void pair_kernel(PairArgs a, Rows of,
   add_up<kPairThreads>(total, part, &last);
 }
 
-constexpr int kMaxRows = 1 << 24;
+constexpr int kMaxRows = (1 << 22) - 1;  // a launch has less than 2^32 lanes, a row's or pair's workgroup up to 1024
 bool valid_logits(const zb_logits* x) {
   if (!x || x->rows < 0 || x->rows > kMaxRows || x->vocab < 1 || x->vocab > kEmbeddingMaxVocab || x->row_stride < x->vocab) return false;
   if (x->row_stride > (int64_t)1 << 32 || (x->dtype != ZB_FP32 && x->dtype != ZB_BF16)) return false;
@@ -690,10 +690,14 @@ hipError_t launch_policy(const zb_logits* x, const Rows& of, const RowOut& out, 
 template <typename T>
 hipError_t launch_grad(const zb_logits* x, const Rows& of, const float* coef, const float* top, const float* inv, void* d, int64_t stride, hipStream_t s) {
   const int per = kThreads * kGradVectors, vectors = x->vocab / Span<T>::VE, parts = vectors > per ? (vectors + per - 1) / per : 1;
-  if ((int64_t)x->rows * parts > 0x7FFFFFFF) return hipErrorInvalidValue;  // (more logits than any memory holds)
-  ZB_NT((grad_kernel<T, NT><<<(unsigned)x->rows * (unsigned)parts, kThreads, 0, s>>>((const T*)x->logits, x->row_stride, of, coef, top, inv, (T*)d,
-                                                                                     stride, parts)));
-  return hipGetLastError();
+  const int most = (int)((1LL << 32) / kThreads - 1) / parts;  // rows of a launch
+  for (int row0 = 0; row0 < x->rows; row0 += most) {
+    const unsigned wgs = (unsigned)(x->rows - row0 < most ? x->rows - row0 : most) * (unsigned)parts;
+    ZB_NT((grad_kernel<T, NT><<<wgs, kThreads, 0, s>>>((const T*)x->logits, x->row_stride, of, coef, top, inv, (T*)d, stride, parts, row0)));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 hipError_t launch_grad(const zb_logits* x, const Rows& of, const float* coef, const float* top, const float* inv, void* d, int64_t stride, hipStream_t s) {
   return x->dtype == ZB_BF16 ? launch_grad<bf16_t>(x, of, coef, top, inv, d, stride, s) : launch_grad<float>(x, of, coef, top, inv, d, stride, s);

@@ -158,3 +158,18 @@ def test_loss_configurations_of_a_stage():
                 dict(loss=1, clip_low=1.5), dict(loss=1, clip_high=inf), dict(loss=1, kl_coef=-1.0), dict(loss=1, kl_coef=nan), dict(loss=2, pref_beta=inf),
                 dict(loss=2, label_smoothing=1.5), dict(loss=2, label_smoothing=nan)):
         assert rc(**bad)[0] == zb.EINVAL, bad
+
+
+def test_more_rows_or_pairs_than_a_launch_holds():
+    """A workgroup of up to 1024 lanes a row, and a launch has less than 2^32 lanes."""
+    most = (1 << 22) - 1
+    x = good_logits(rows=most + 1)
+    assert rc_of(zb.token_logprobs, x, AT) == zb.EINVAL
+    assert rc_of(zb.token_logprobs_backward, x, AT, AT, AT) == zb.EINVAL
+    ws = dict(workspace=AT, workspace_bytes=1 << 40)
+    assert rc_of(zb.policy_loss, x, zb.policy(AT, AT), AT, AT, AT, **ws) == zb.EINVAL
+    for pairs in (9, most + 1):
+        assert rc_of(zb.preference_loss, x if pairs == 9 else good_logits(), zb.preference(AT, AT, pairs), AT, AT, AT, AT, **ws) == zb.EINVAL
+    for rows, pairs in ((most + 1, 0), (0, most + 1)):
+        assert rc_of(zb.loss_workspace_bytes, rows, pairs) == zb.EINVAL
+    assert zb.loss_workspace_bytes(most, most) > 0
