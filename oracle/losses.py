@@ -80,7 +80,8 @@ def preference(z, targets, ref, offsets, weight=None, beta=0.1, eps=0.0, scale=1
     loss, c = 0.0, np.zeros(len(targets))
     for i in range(len(sums) // 2):
         x = beta * (sums[2 * i] - sums[2 * i + 1])
-        loss += scale * ((1 - eps) * np.logaddexp(0, -x) + eps * np.logaddexp(0, x))
+        for share, y in ((1 - eps, -x), (eps, x)):  # (a share of 0 takes nothing of an infinite term)
+            loss += scale * share * np.logaddexp(0, y) if share else 0.0
         slope = scale * beta * (eps * np.exp(-np.logaddexp(0, -x)) - (1 - eps) * np.exp(-np.logaddexp(0, x)))
         for q, sign in ((2 * i, 1), (2 * i + 1, -1)):
             c[offsets[q]:offsets[q + 1]] = sign * slope * w[offsets[q]:offsets[q + 1]]

@@ -583,7 +583,9 @@ __global__ __launch_bounds__(kPairThreads) void pair_kernel(PairArgs a, Rows of,
       if (rewards) rewards[2 * blockIdx.x + q] = (float)(a.beta * s[q]);
     }
     const double x = a.beta * (s[0] - s[1]), e = exp(-fabs(x)), l = log1p(e);  // -log sigma(x) = max(-x, 0) + l
-    loss = a.scale * ((1.0 - a.smoothing) * (fmax(-x, 0.0) + l) + a.smoothing * (fmax(x, 0.0) + l));
+    // (x may be infinite: a share of 0 takes nothing of an infinite term)
+    const double kept = 1.0 - a.smoothing;
+    loss = a.scale * ((kept != 0.0 ? kept * (fmax(-x, 0.0) + l) : 0.0) + (a.smoothing != 0.0 ? a.smoothing * (fmax(x, 0.0) + l) : 0.0));
     const double above = x >= 0 ? 1.0 / (1.0 + e) : e / (1.0 + e);  // sigma(x)
     const double below = x >= 0 ? e / (1.0 + e) : 1.0 / (1.0 + e);  // sigma(-x)
     slope_of = a.grad_scale * a.beta * (a.smoothing * above - (1.0 - a.smoothing) * below);
