@@ -26,11 +26,11 @@ def _blocks(x):
     return np.concatenate([x, np.zeros(pad)]).reshape(-1, BLOCK)
 
 
-def encode(x, most, power, least, u):
-    """(codes with the sign of x, tops in fp32) of the values x."""
+def encode(x, most, power, least, u, top=None):
+    """(codes with the sign of x, tops in fp32) of the values x; top: scales to use instead of the blocks' own."""
     n = len(x)
     b = _blocks(np.asarray(x, np.float64))
-    top = np.abs(b).max(axis=1).astype(np.float32)
+    top = np.abs(b).max(axis=1).astype(np.float32) if top is None else top
     unit = np.repeat(top.astype(np.float64), BLOCK)[:n] / float(most) ** power
     y = np.abs(np.asarray(x, np.float64))
     ladder = np.arange(most + 2, dtype=np.float64) ** power

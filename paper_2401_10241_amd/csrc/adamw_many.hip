@@ -129,6 +129,9 @@ __device__ __forceinline__ void move_theta_near(float& th, float m, float v, con
 
 constexpr double kUnitM = 1.0 / (127.0 * 127.0), kUnitV = 1.0 / (255.0 * 255.0 * 255.0 * 255.0);
 constexpr float kMostFloat = 3.4028235e38f;
+// Whether a block's scale is off its largest value by more than half a step of 24 bits: cut off at the largest float, or subnormal (not 0).  Then
+// values lie past the top code.
+__device__ __forceinline__ bool coarse(float top) { return top >= kMostFloat || __float_as_uint(top) - 1u < 0x007FFFFFu; }
 // c^4 for c <= 256 in products of 24 bits (256^4 wraps to 0, which differences of neighbours put right again)
 __device__ __forceinline__ unsigned fourth(unsigned c) {
   c &= 0x1FFu;
@@ -155,7 +158,7 @@ struct Places {  // of four values one after the other
 // Code of |m|: y = |m| / unit lies between c^2 and (c + 1)^2, and the upper code is taken if n / 131072 of the way is less than y - c^2
 // (n = 65536: the nearer one).  c comes from the root in 32 bits, which may be on the wrong side of a whole number by
 // 127 * 1.5 * 2^-23 at most: then y is that near to a code, and only an n within 3 of 0 or 131072 could take another one.  SURE sets c
-// right first, for those (risky()) and for values past the block's largest.
+// right first, for those (risky()) and for blocks whose values may lie past the top code (coarse()).
 template <bool SURE> __device__ __forceinline__ unsigned encode_m(double m, double inv, unsigned n) {
   const double y = fabs(m) * inv;
   int c = (int)__builtin_amdgcn_sqrtf((float)y);
@@ -166,7 +169,7 @@ template <bool SURE> __device__ __forceinline__ unsigned encode_m(double m, doub
   }
   const double r = fma(-(double)c, (double)c, y);
   const unsigned w = 2 * (unsigned)c + 1;
-  if ((double)((n & 0x3FFFFu) * (w & 0xFFu)) < r * 131072.0 && (!SURE || c < 127)) ++c;  // (at 127, r is too small unless SURE)
+  if ((double)((n & 0x3FFFFu) * (w & 0xFFu)) < r * 131072.0 && (!SURE || c < 127)) ++c;  // (at 127, r < 2^-23 y unless coarse(), too little for any n)
   return (unsigned)(m < 0 ? -c : c) & 0xFFu;
 }
 // The same for v between c^4 and (c + 1)^4, where the root of the root is off by 255 * 1.6 * 2^-23 at most and n within 6; a positive v has
@@ -343,7 +346,7 @@ template <bool BITS8, bool WHOLE, bool NT> struct Four {
     unsigned wm, wv;
     Ends ends;
     encode_four<false>(m64, v64, im, iv, at, &ends, &wm, &wv);
-    if (ends.risky() || top_m >= kMostFloat || top_v >= kMostFloat) encode_four<true>(m64, v64, im, iv, at, &ends, &wm, &wv);
+    if (ends.risky() || coarse(top_m) || coarse(top_v)) encode_four<true>(m64, v64, im, iv, at, &ends, &wm, &wv);
     store_codes<NT>(q.m, i, live, wide, wm);
     store_codes<NT>(q.v, i, live, wide, wv);
     if (in && (threadIdx.x & 63) == 0) { q.m_scale[i / kBlock] = top_m; q.v_scale[i / kBlock] = top_v; }
