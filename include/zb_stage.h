@@ -423,7 +423,9 @@ typedef struct {
 typedef struct {
   int32_t bits;       /* 8 or 32 */
   uint32_t seed;
-  double beta1, beta2, eps, weight_decay;
+  double beta1, beta2; /* in (0, 1) */
+  double eps;         /* 32 bits in the kernels, as weight_decay and lr are: at least the smallest normal float, 1.18e-38 */
+  double weight_decay;
   double clip;        /* threshold of the gradient norm, > 0; infinity: none */
 } zb_adamw_config;
 

@@ -641,9 +641,9 @@ zb_status zb_adamw_step(const zb_adamw_config* cfg, const zb_adamw_tensor* tenso
                         const int32_t* nonfinite, void* hip_stream) {
   if (!cfg || !valid_tensors(tensors, count) || !state || misaligned(state, 8)) return ZB_EINVAL;
   if (cfg->bits != 8 && cfg->bits != 32) return ZB_EINVAL;
-  if (!(cfg->beta1 > 0 && cfg->beta1 < 1 && cfg->beta2 > 0 && cfg->beta2 < 1 && cfg->eps > 0 && cfg->clip > 0) || !isfinite(cfg->eps) ||
-      !isfinite(cfg->weight_decay) || !isfinite(lr))
-    return ZB_EINVAL;
+  if (!(cfg->beta1 > 0 && cfg->beta1 < 1 && cfg->beta2 > 0 && cfg->beta2 < 1 && cfg->clip > 0)) return ZB_EINVAL;
+  // as the kernels use them; eps is divided by where a value has had no gradient, with a reciprocal that takes normal numbers
+  if (!((float)cfg->eps >= 1.17549435e-38f) || !isfinite((float)cfg->eps) || !isfinite((float)cfg->weight_decay) || !isfinite((float)lr)) return ZB_EINVAL;
   if ((sq == nullptr) != (nonfinite == nullptr) || misaligned(sq, 8) || misaligned(nonfinite, 4)) return ZB_EINVAL;
   if (cfg->bits == 8 && !sq) return ZB_EINVAL;  // codes cannot hold a NaN
   for (int32_t k = 0; k < count; ++k) {
