@@ -122,7 +122,9 @@ __device__ __forceinline__ void move_theta(float& th, float m, float v, const Hy
 }
 
 // The same with the hardware's root and reciprocal, each off by one unit in the last place: 8-bit states are bound by instructions, and
-// their m and v come from 64 bits, so the update stays as exact as the other.
+// their m and v come from 64 bits, so the update stays as exact as the other.  The root takes a v / bc2 below 2^-126 for 0, 1.09e-19 less than it
+// is, so an eps below kNearEps, of which that is more than half a step, takes move_theta.
+constexpr float kNearEps = 2e-12f;
 __device__ __forceinline__ void move_theta_near(float& th, float m, float v, const Hyper& hp, float decay, float ib1, float ib2) {
   th = th - hp.lr * (decay * th + (m * ib1) * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v * ib2) + hp.eps));
 }
@@ -294,7 +296,7 @@ template <bool BITS8, bool WHOLE, bool NT> struct Four {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       float x = th[e];
-      if (BITS8) move_theta_near(x, m[e], v[e], hp, decay, clk.ib1, clk.ib2);
+      if (BITS8 && hp.eps >= kNearEps) move_theta_near(x, m[e], v[e], hp, decay, clk.ib1, clk.ib2);
       else move_theta(x, m[e], v[e], hp, decay, clk.bc1, clk.bc2);
       th[e] = x;
     }
