@@ -359,9 +359,10 @@ typedef struct {
 zb_status zb_token_logprobs(const zb_logits* x, float* logp, float* lse, void* hip_stream);
 
 /* dlogits[r, j] = dlogp[r] * ([j == targets[r]] - exp(logits[r, j] - lse[r])), with zb_token_logprobs' lse.  A row
- * whose dlogp is 0 is not read and gets zeros.  dlogits may be the logits themselves (then with the same stride,
- * ZB_EINVAL otherwise) and must not overlap them in any other way; dlogits_stride 0 stands for x->row_stride.  Only
- * [rows, vocab] is written. */
+ * whose dlogp is 0 is not read and gets zeros.  The probabilities carry the rounding of the fp32 lse, a share of up to
+ * 2^-24 |lse| of themselves, and so does 1 - p of the target (the two losses below take it from the sums, in more bits).
+ * dlogits may be the logits themselves (then with the same stride, ZB_EINVAL otherwise) and must not overlap them in any other
+ * way; dlogits_stride 0 stands for x->row_stride.  Only [rows, vocab] is written. */
 zb_status zb_token_logprobs_backward(const zb_logits* x, const float* lse, const float* dlogp, void* dlogits,
                                      int64_t dlogits_stride, void* hip_stream);
 

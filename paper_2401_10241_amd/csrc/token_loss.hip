@@ -1,6 +1,8 @@
 // Losses on the log-probabilities of given tokens, and the gradient of the logits they come from: with
 //   lse_r = log sum_j exp(z_rj),  logp_r = z_r,target(r) - lse_r,  c_r = d(loss) / d(logp_r)
 // every loss here has  d(loss) / d(z_rj) = c_r ([j = target(r)] - exp(z_rj - lse_r)).
+// The target's entry is c_r (1 - p), p its probability: 1 - p comes from the other tokens' exponentials, which are added up without the target's, and so
+// does log p where the target has nearly all of the row.
 // A row counts if its target lies in [0, vocab), its weight is not zero and, where there are sequences, one of them holds it;
 // the logits of the others are not read.
 #include <math.h>
@@ -42,6 +44,8 @@ template <typename T> struct Span {
     if (lane < VE) return lane < head ? lane : -1;
     return lane - VE < tail ? head + full * VE + lane - VE : -1;  // (tail < VE: lanes from 2 VE on have none)
   }
+  // the vector that element j is in, -1 if it lies beside them
+  __device__ __forceinline__ int vector_of(int j) const { return j >= head && j < head + full * VE ? (j - head) / VE : -1; }
 };
 template <typename T> __device__ __forceinline__ void unpack(const uint4& r, float (&x)[16 / sizeof(T)]);
 template <> __device__ __forceinline__ void unpack<float>(const uint4& r, float (&x)[4]) {
@@ -66,24 +70,40 @@ template <typename T> __device__ __forceinline__ uint4 empty_pack();  // all -in
 template <> __device__ __forceinline__ uint4 empty_pack<float>() { return make_uint4(0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u); }
 template <> __device__ __forceinline__ uint4 empty_pack<bf16_t>() { return make_uint4(0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u); }
 
+// A vector whose element e is -infinity.
+template <typename T> __device__ __forceinline__ uint4 without(const uint4& r, int e);
+template <> __device__ __forceinline__ uint4 without<float>(const uint4& r, int e) {
+  const unsigned none = 0xFF800000u;
+  return make_uint4(e == 0 ? none : r.x, e == 1 ? none : r.y, e == 2 ? none : r.z, e == 3 ? none : r.w);
+}
+template <> __device__ __forceinline__ uint4 without<bf16_t>(const uint4& r, int e) {
+  unsigned w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (i == e >> 1) w[i] = e & 1 ? (w[i] & 0xFFFFu) | 0xFF800000u : (w[i] & 0xFFFF0000u) | 0xFF80u;
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // Keeps a row as it was loaded: without it the 32-bit forms of one pass over it are kept for the next, in twice the registers.
 template <int NV> __device__ __forceinline__ void as_loaded(uint4 (&r)[NV]) {
 #pragma unroll
   for (int i = 0; i < NV; ++i) asm volatile("" : "+v"(r[i].x), "+v"(r[i].y), "+v"(r[i].z), "+v"(r[i].w));
 }
 
-__device__ __forceinline__ float exp_of(float x, float top) { return __builtin_amdgcn_exp2f((x - top) * kLog2e); }
-// The same for sums over a row, without the bias of a log2(e) of 24 bits: log-probabilities are added over sequences, where errors of one sign
-// would add up while the values cancel.
-__device__ __forceinline__ float exp_for_sum(float x, float top) {
+// exp(x - top), without the bias of a log2(e) of 24 bits: log-probabilities are added over sequences, where errors of one sign would add up
+// while the values cancel.  (What is left is the exponent's rounding, 2^-24 (x - top) of the result in either direction.)
+__device__ __forceinline__ float exp_of(float x, float top) {
   const float d = x - top;
   return __builtin_amdgcn_exp2f(fmaf(d, kLog2e, d * 1.925963033e-8f));
 }
+// The same for an entry of a gradient of type T: stored in bf16, the bias (a share of 2e-8 (x - top)) is far below half a step, 2^-8.
+template <typename T> __device__ __forceinline__ float exp_in(float x, float top) { return exp_of(x, top); }
+template <> __device__ __forceinline__ float exp_in<bf16_t>(float x, float top) { return __builtin_amdgcn_exp2f((x - top) * kLog2e); }
 // Sum of a vector's exponentials.  Vectors are added up in 64 bits: one large term would round off a part of each small one that follows it.
 template <int VE> __device__ __forceinline__ double exp_sum(const float (&x)[VE], float top) {
   float t[VE];
 #pragma unroll
-  for (int e = 0; e < VE; ++e) t[e] = exp_for_sum(x[e], top);
+  for (int e = 0; e < VE; ++e) t[e] = exp_of(x[e], top);
 #pragma unroll
   for (int w = VE / 2; w > 0; w /= 2)
 #pragma unroll
@@ -253,20 +273,24 @@ template <int THREADS> __device__ __forceinline__ void add_up(const Total& t, co
 struct RowOut {  // what the row kernels leave of a row; null: not wanted
   float *logp, *lse;
   float *top, *inv;  // p_j = exp(z_j - top) * inv
+  float* miss;       // 1 - p of the target
   double *logp64;    // logp before its rounding
   double* part;      // with a policy: its loss
   Total total;
 };
-__device__ __forceinline__ void put_row(const RowOut& o, int row, double logp, double lse, float top, float s) {
+__device__ __forceinline__ void put_row(const RowOut& o, int row, double logp, double lse, float top, float s, float others) {
   if (o.logp) o.logp[row] = (float)logp;
   if (o.lse) o.lse[row] = (float)lse;
-  if (o.top) { o.top[row] = top; o.inv[row] = 1.0f / s; }
+  if (o.top) {
+    const float inv = 1.0f / s;
+    o.top[row] = top; o.inv[row] = inv; o.miss[row] = others * inv;
+  }
   if (o.logp64) o.logp64[row] = logp;
 }
 __device__ __forceinline__ void put_no_row(const RowOut& o, int row) {
   if (o.logp) o.logp[row] = 0.f;
   if (o.lse) o.lse[row] = 0.f;
-  if (o.top) { o.top[row] = 0.f; o.inv[row] = 0.f; }
+  if (o.top) { o.top[row] = 0.f; o.inv[row] = 0.f; o.miss[row] = 0.f; }
   if (o.logp64) o.logp64[row] = 0.0;
 }
 
@@ -300,11 +324,15 @@ __device__ __forceinline__ void policy_in_registers(const T* logits, long stride
     const int k = i * THREADS + lane;
     r[i] = k < sp.full ? get16<NT>(v + k) : empty_pack<T>();
   }
-  const int edge = sp.edge(lane);
-  const float xe = edge >= 0 ? to_f32(z[edge]) : -INFINITY;
-  const int target = of.targets[row];
-  const float zy = to_f32(z[target]);
+  const int edge = sp.edge(lane), target = of.targets[row], vt = sp.vector_of(target);
+  const float xe = edge >= 0 && edge != target ? to_f32(z[edge]) : -INFINITY, zy = to_f32(z[target]);
   if (lane == 0) in = terms_of(pol, of, row);  // (on their way with the row; kept apart from it, whose lanes have no registers to spare)
+  const bool owner = vt < 0 ? edge == target : vt % THREADS == lane;  // the lane whose entry the target is; it keeps it apart from the others
+  if (owner) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (i * THREADS + lane == vt) r[i] = without<T>(r[i], (target - sp.head) % VE);
+  }
   float m = xe;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -313,29 +341,29 @@ __device__ __forceinline__ void policy_in_registers(const T* logits, long stride
 #pragma unroll
     for (int e = 0; e < VE; ++e) m = fmaxf(m, x[e]);
   }
-  m = block_max<N>(m, red_m);
+  m = fmaxf(block_max<N>(m, red_m), zy);
   as_loaded(r);
-  double acc = (double)exp_for_sum(xe, m);  // (a NaN, an infinity and a row of nothing but -infinity make the sum NaN)
+  double acc = (double)exp_of(xe, m);  // (a NaN, an infinity and a row of nothing but -infinity make the sum NaN)
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     float x[VE];
     unpack<T>(r[i], x);
     acc += exp_sum<VE>(x, m);
   }
-  const double s64 = block_sum<N>(acc, red_s);
-  const float s = (float)s64;
+  const double rest = block_sum<N>(acc, red_s), s64 = rest + (double)exp_of(zy, m);
+  const float s = (float)s64, others = (float)rest;
   double loss = 0.0;
   if (lane == 0) {
     const double l = log_of(s64), lp = ((double)zy - (double)m) - l;
     double slope;
     loss = policy_row(pol, in, lp, &slope);
-    put_row(out, row, lp, (double)m + l, m, s);
+    put_row(out, row, lp, (double)m + l, m, s, others);
     coef_of = (float)slope;
   }
   if (dlogits) __syncthreads();
   if (lane == 0) announce(out.total, out.part, loss, last);
   if (!dlogits) return;
-  const float coef = coef_of, neg = -coef / s;
+  const float coef = coef_of, inv = 1.f / s, neg = -coef * inv;
   if (coef == 0.f) {
     clear_row<T, NT>(d, of.vocab, THREADS);
     return;
@@ -349,7 +377,7 @@ __device__ __forceinline__ void policy_in_registers(const T* logits, long stride
     float x[VE];
     unpack<T>(r[i], x);
 #pragma unroll
-    for (int e = 0; e < VE; ++e) x[e] = neg * exp_of(x[e], m);
+    for (int e = 0; e < VE; ++e) x[e] = neg * exp_in<T>(x[e], m);
     T* at = d + sp.head + k * VE;
     if (same) {
       put16<NT>(at, pack<T>(x));
@@ -358,10 +386,8 @@ __device__ __forceinline__ void policy_in_registers(const T* logits, long stride
       for (int e = 0; e < VE; ++e) at[e] = from_f32<T>(x[e]);
     }
   }
-  if (edge >= 0) d[edge] = from_f32<T>(neg * exp_of(xe, m));
-  // the lane that wrote the target's entry writes it again, whole
-  const int kt = target - sp.head;
-  if (kt >= 0 && kt < sp.full * VE ? (kt / VE) % THREADS == lane : edge == target) d[target] = from_f32<T>(coef * (1.f - exp_of(zy, m) / s));
+  if (edge >= 0) d[edge] = from_f32<T>(neg * exp_in<T>(xe, m));
+  if (owner) d[target] = from_f32<T>(coef * (others * inv));  // (the lane that wrote the vector around it)
 }
 template <typename T, int THREADS, int NV, int WAVES, bool NT>
 __global__ __launch_bounds__(THREADS, WAVES) void policy_row_kernel(const T* logits, long stride, Rows of, RowOut out, PolicyArgs pol, T* dlogits,
@@ -392,8 +418,10 @@ __device__ __forceinline__ void row_in_passes(const T* logits, long stride, Rows
   const T* z = logits + (long)row * stride;
   const Span<T> sp(z, of.vocab);
   const uint4* v = reinterpret_cast<const uint4*>(z + sp.head);
-  const int edge = sp.edge(lane), target = of.targets[row];
-  const float xe = edge >= 0 ? to_f32(z[edge]) : -INFINITY, zy = to_f32(z[target]);
+  const int edge = sp.edge(lane), target = of.targets[row], vt = sp.vector_of(target);
+  const bool owner = vt < 0 ? edge == target : vt % THREADS == lane;  // the lane whose entry the target is; it keeps it apart from the others
+  const int own_vector = owner ? vt : -1;
+  const float xe = edge >= 0 && edge != target ? to_f32(z[edge]) : -INFINITY, zy = to_f32(z[target]);
   float mine = xe;
   double part = edge >= 0 ? 1.0 : 0.0;  // the lane's sum counts exp(x - mine)
   if (xe != xe) part = (double)xe;
@@ -401,6 +429,11 @@ __device__ __forceinline__ void row_in_passes(const T* logits, long stride, Rows
     uint4 r[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) r[i] = k0 + i * THREADS < sp.full ? get16<NT>(v + k0 + i * THREADS) : empty_pack<T>();
+    if (own_vector >= k0 && own_vector < k0 + U * THREADS) {
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+        if (k0 + i * THREADS == own_vector) r[i] = without<T>(r[i], (target - sp.head) % VE);
+    }
     float top = mine;
 #pragma unroll
     for (int i = 0; i < U; ++i) {
@@ -410,7 +443,7 @@ __device__ __forceinline__ void row_in_passes(const T* logits, long stride, Rows
       for (int e = 0; e < VE; ++e) top = fmaxf(top, x[e]);
     }
     if (top > mine) {
-      part = mine == -INFINITY ? (part != part ? part : 0.0) : part * (double)exp_for_sum(mine, top);
+      part = mine == -INFINITY ? (part != part ? part : 0.0) : part * (double)exp_of(mine, top);
       mine = top;
     }
 #pragma unroll
@@ -425,11 +458,11 @@ __device__ __forceinline__ void row_in_passes(const T* logits, long stride, Rows
       }
     }
   }
-  const float m = block_max<N>(mine, red_m);
+  const float m = fmaxf(block_max<N>(mine, red_m), zy);
   // lanes without a finite logit add nothing, unless they saw a NaN; a row without one is undefined
-  const double own = mine == -INFINITY && m > -INFINITY ? (part != part ? part : 0.0) : part * (double)exp_for_sum(mine, m);
-  const double s64 = block_sum<N>(own, red_s);
-  const float s = (float)s64;
+  const double own = mine == -INFINITY && m > -INFINITY ? (part != part ? part : 0.0) : part * (double)exp_of(mine, m);
+  const double rest = block_sum<N>(own, red_s), s64 = rest + (double)exp_of(zy, m);
+  const float s = (float)s64, others = (float)rest;
   double loss = 0.0;
   if (lane == 0) {
     const double l = log_of(s64), lp = ((double)zy - (double)m) - l;
@@ -438,13 +471,13 @@ __device__ __forceinline__ void row_in_passes(const T* logits, long stride, Rows
       loss = policy_row(pol, terms_of(pol, of, row), lp, &slope);
       coef_of = (float)slope;
     }
-    put_row(out, row, lp, (double)m + l, m, s);
+    put_row(out, row, lp, (double)m + l, m, s, others);
   }
   if (!POLICY) return;
   if (dlogits) __syncthreads();
   if (lane == 0) announce(out.total, out.part, loss, last);
   if (!dlogits) return;
-  const float coef = coef_of, neg = -coef / s;
+  const float coef = coef_of, inv = 1.f / s, neg = -coef * inv;
   if (coef == 0.f) {
     clear_row<T, NT>(d, of.vocab, THREADS);
     return;
@@ -454,7 +487,7 @@ __device__ __forceinline__ void row_in_passes(const T* logits, long stride, Rows
     float x[VE];
     unpack<T>(get16<NT>(v + k), x);
 #pragma unroll
-    for (int e = 0; e < VE; ++e) x[e] = neg * exp_of(x[e], m);
+    for (int e = 0; e < VE; ++e) x[e] = neg * exp_in<T>(x[e], m);
     T* at = d + sp.head + k * VE;
     if (same) {
       put16<NT>(at, pack<T>(x));
@@ -463,9 +496,8 @@ __device__ __forceinline__ void row_in_passes(const T* logits, long stride, Rows
       for (int e = 0; e < VE; ++e) at[e] = from_f32<T>(x[e]);
     }
   }
-  if (edge >= 0) d[edge] = from_f32<T>(neg * exp_of(xe, m));
-  const int kt = target - sp.head;
-  if (kt >= 0 && kt < sp.full * VE ? (kt / VE) % THREADS == lane : edge == target) d[target] = from_f32<T>(coef * (1.f - exp_of(zy, m) / s));
+  if (edge >= 0) d[edge] = from_f32<T>(neg * exp_in<T>(xe, m));
+  if (owner) d[target] = from_f32<T>(coef * (others * inv));  // (the lane that wrote the vector around it)
 }
 template <typename T, int THREADS, int U, bool POLICY, bool NT>
 __global__ __launch_bounds__(THREADS) void row_kernel(const T* logits, long stride, Rows of, RowOut out, PolicyArgs pol, T* dlogits, long dstride) {
@@ -474,15 +506,15 @@ __global__ __launch_bounds__(THREADS) void row_kernel(const T* logits, long stri
   if (POLICY) add_up<THREADS>(out.total, out.part, &last);
 }
 
-// coef ([j = target] - exp(z_j - top) inv), inv null: 1, by workgroups of kThreads * kGradVectors vectors of a row.  Bound by HBM: the rows of
+// coef ([j = target] - exp(z_j - top) inv), inv null: 1, with the target's 1 - p from `misses` where there are any, by workgroups of kThreads * kGradVectors vectors of a row.  Bound by HBM: the rows of
 // six pairs of about 500 tokens x 50432 bf16, which have just been read for their log-probabilities, 144 us = 6.8 TB/s with the
 // rows without weight, which are not read.  us of log-probabilities and gradient with 2 / 4 / 8 vectors a lane: 229 / 239 / 258; from the
 // last row to the first, towards what the caches may still hold: 239.
 constexpr int kGradVectors = 2;
 template <typename T, bool NT>
 __global__ __launch_bounds__(kThreads) void grad_kernel(const T* logits, long stride, Rows of, const float* __restrict__ coefs,
-                                                        const float* __restrict__ tops, const float* __restrict__ invs, T* dlogits, long dstride,
-                                                        int parts, int row0) {
+                                                        const float* __restrict__ tops, const float* __restrict__ invs,
+                                                        const float* __restrict__ misses, T* dlogits, long dstride, int parts, int row0) {
   constexpr int VE = Span<T>::VE;
   const int at_row = blockIdx.x / parts, part = blockIdx.x - at_row * parts, row = row0 + at_row, lane = threadIdx.x;
   const float coef = of.counts(row) ? coefs[row] : 0.f;
@@ -507,7 +539,7 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(const T* logits, long st
     if (edge >= 0) d[edge] = from_f32<T>(0.f);
     return;
   }
-  const float top = tops[row], inv = invs ? invs[row] : 1.f, neg = -coef * inv;
+  const float top = tops[row], inv = invs ? invs[row] : 1.f, miss = misses ? misses[row] : 0.f, neg = -coef * inv;
   const int target = of.targets[row];
   const uint4* v = reinterpret_cast<const uint4*>(z + sp.head);
   uint4 r[kGradVectors];
@@ -529,7 +561,7 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(const T* logits, long st
       for (int e = 0; e < VE; ++e) if (j + e == target) y = x[e];
     }
 #pragma unroll
-    for (int e = 0; e < VE; ++e) x[e] = neg * exp_of(x[e], top);
+    for (int e = 0; e < VE; ++e) x[e] = neg * exp_in<T>(x[e], top);
     T* at = d + j;
     if (same) {
       put16<NT>(at, pack<T>(x));
@@ -537,11 +569,11 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(const T* logits, long st
 #pragma unroll
       for (int e = 0; e < VE; ++e) at[e] = from_f32<T>(x[e]);
     }
-    if (hot) d[target] = from_f32<T>(coef * (1.f - exp_of(y, top) * inv));
+    if (hot) d[target] = from_f32<T>(coef * (misses ? miss : 1.f - exp_of(y, top) * inv));
   }
   if (edge >= 0) {
     const float p = exp_of(to_f32(z[edge]), top) * inv;
-    d[edge] = from_f32<T>(edge == target ? coef * (1.f - p) : -coef * p);
+    d[edge] = from_f32<T>(edge == target ? coef * (misses ? miss : 1.f - p) : -coef * p);
   }
 }
 
@@ -613,10 +645,10 @@ bool valid_dlogits(const zb_logits* x, const void* d, int64_t* stride) {
 }
 bool misaligned(const void* p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
 
-struct Workspace {  // a counter; per row a partial loss, the log-probability, what makes probabilities of logits, the coefficient
+struct Workspace {  // a counter; per row a partial loss, the log-probability, what makes probabilities of logits, the target's 1 - p, the coefficient
   unsigned* done;
   double *part, *logp;
-  float *top, *inv, *coef;
+  float *top, *inv, *miss, *coef;
 };
 Workspace carve(void* base, int rows, int pairs) {
   Workspace w;
@@ -625,7 +657,8 @@ Workspace carve(void* base, int rows, int pairs) {
   w.logp = w.part + (rows > pairs ? rows : pairs);
   w.top = (float*)(w.logp + rows);
   w.inv = w.top + rows;
-  w.coef = w.inv + rows;
+  w.miss = w.inv + rows;
+  w.coef = w.miss + rows;
   return w;
 }
 
@@ -690,19 +723,22 @@ hipError_t launch_policy(const zb_logits* x, const Rows& of, const RowOut& out, 
   return hipGetLastError();
 }
 template <typename T>
-hipError_t launch_grad(const zb_logits* x, const Rows& of, const float* coef, const float* top, const float* inv, void* d, int64_t stride, hipStream_t s) {
+hipError_t launch_grad(const zb_logits* x, const Rows& of, const float* coef, const float* top, const float* inv, const float* miss, void* d, int64_t stride,
+                       hipStream_t s) {
   const int per = kThreads * kGradVectors, vectors = x->vocab / Span<T>::VE, parts = vectors > per ? (vectors + per - 1) / per : 1;
   const int most = (int)((1LL << 32) / kThreads - 1) / parts;  // rows of a launch
   for (int row0 = 0; row0 < x->rows; row0 += most) {
     const unsigned wgs = (unsigned)(x->rows - row0 < most ? x->rows - row0 : most) * (unsigned)parts;
-    ZB_NT((grad_kernel<T, NT><<<wgs, kThreads, 0, s>>>((const T*)x->logits, x->row_stride, of, coef, top, inv, (T*)d, stride, parts, row0)));
+    ZB_NT((grad_kernel<T, NT><<<wgs, kThreads, 0, s>>>((const T*)x->logits, x->row_stride, of, coef, top, inv, miss, (T*)d, stride, parts, row0)));
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
 }
-hipError_t launch_grad(const zb_logits* x, const Rows& of, const float* coef, const float* top, const float* inv, void* d, int64_t stride, hipStream_t s) {
-  return x->dtype == ZB_BF16 ? launch_grad<bf16_t>(x, of, coef, top, inv, d, stride, s) : launch_grad<float>(x, of, coef, top, inv, d, stride, s);
+hipError_t launch_grad(const zb_logits* x, const Rows& of, const float* coef, const float* top, const float* inv, const float* miss, void* d, int64_t stride,
+                       hipStream_t s) {
+  return x->dtype == ZB_BF16 ? launch_grad<bf16_t>(x, of, coef, top, inv, miss, d, stride, s)
+                             : launch_grad<float>(x, of, coef, top, inv, miss, d, stride, s);
 }
 zb_status said(hipError_t e) { return e == hipSuccess ? ZB_OK : ZB_EDEVICE; }
 
@@ -710,7 +746,7 @@ zb_status said(hipError_t e) { return e == hipSuccess ? ZB_OK : ZB_EDEVICE; }
 
 size_t loss_workspace_bytes(int rows, int pairs) {
   const size_t n = (size_t)(rows > pairs ? rows : pairs);
-  return n * sizeof(double) + (size_t)rows * (sizeof(double) + 3 * sizeof(float)) + 256;
+  return n * sizeof(double) + (size_t)rows * (sizeof(double) + 4 * sizeof(float)) + 256;
 }
 
 bool valid_policy(const zb_policy* p) {
@@ -759,7 +795,7 @@ zb_status preference_loss(const zb_logits* x, const zb_preference* p, double gra
   const Rows of{x->targets, p->weight, p->pairs ? p->offsets : nullptr, p->pairs ? 2 * p->pairs : -1, x->vocab};
   if (x->rows) {
     RowOut out{logp};
-    out.top = w.top; out.inv = w.inv; out.logp64 = w.logp;
+    out.top = w.top; out.inv = w.inv; out.miss = w.miss; out.logp64 = w.logp;
     if (launch_logp(x, of, out, !dlogits && past_caches(x), s) != hipSuccess) return ZB_EDEVICE;
   }
   if (p->pairs) {
@@ -767,7 +803,7 @@ zb_status preference_loss(const zb_logits* x, const zb_preference* p, double gra
     pair_kernel<<<p->pairs, kPairThreads, 0, s>>>(a, of, x->rows, w.logp, rewards, w.coef, w.part, p->pairs <= kSumInPlace ? Total{loss, w.done} : Total{});
     if (hipGetLastError() != hipSuccess) return ZB_EDEVICE;
   }
-  if (x->rows && dlogits && launch_grad(x, of, w.coef, w.top, w.inv, dlogits, dlogits_stride, s) != hipSuccess) return ZB_EDEVICE;
+  if (x->rows && dlogits && launch_grad(x, of, w.coef, w.top, w.inv, w.miss, dlogits, dlogits_stride, s) != hipSuccess) return ZB_EDEVICE;
   if (!p->pairs || p->pairs > kSumInPlace) sum_kernel<<<1, 1024, 0, s>>>(w.part, p->pairs, loss);
   return said(hipGetLastError());
 }
@@ -794,7 +830,7 @@ zb_status zb_token_logprobs_backward(const zb_logits* x, const float* lse, const
   if (!lse || !dlogp || !dlogits) return ZB_EINVAL;
   OnDeviceOf on((hipStream_t)hip_stream);
   if (!on.ok) return ZB_EDEVICE;
-  return said(launch_grad(x, Rows{x->targets, nullptr, nullptr, 0, x->vocab}, dlogp, lse, nullptr, dlogits, dlogits_stride, (hipStream_t)hip_stream));
+  return said(launch_grad(x, Rows{x->targets, nullptr, nullptr, 0, x->vocab}, dlogp, lse, nullptr, nullptr, dlogits, dlogits_stride, (hipStream_t)hip_stream));
 }
 
 zb_status zb_loss_workspace_bytes(int32_t rows, int32_t pairs, size_t* bytes) {
