@@ -144,7 +144,7 @@ typedef struct {
                                1 / tokens; with ZB_LOSS_PREFERENCE, zb_preference_loss's with scale 1 / pairs, samples 2i (preferred)
                                and 2i + 1 being a pair (mb_size even).  B starts from the gradient of the mean of LOSS over the
                                iteration's m microbatches; F computes it in the place of the logits and keeps it for B and W, so the
-                               tensors above must be set before F */
+                               tensors above must be set before F.  Both take fewer than 2^22 tokens per microbatch */
   double clip_low, clip_high, kl_coef; /* policy */
   double pref_beta, label_smoothing;   /* preference */
 } zb_config;
@@ -359,8 +359,8 @@ typedef struct {
 zb_status zb_token_logprobs(const zb_logits* x, float* logp, float* lse, void* hip_stream);
 
 /* dlogits[r, j] = dlogp[r] * ([j == targets[r]] - exp(logits[r, j] - lse[r])), with zb_token_logprobs' lse.  A row
- * whose dlogp is 0 is not read and gets zeros.  The probabilities carry the rounding of the fp32 lse, a share of up to
- * 2^-24 |lse| of themselves, and so does 1 - p of the target (the two losses below take it from the sums, in more bits).
+ * whose dlogp is 0 is not read and gets zeros.  The fp32 lse is rounded: by it a probability p is off
+ * by up to 2^-24 |lse| of itself, and the target's 1 - p by that share of p (the two losses below have 1 - p to a share of itself).
  * dlogits may be the logits themselves (then with the same stride, ZB_EINVAL otherwise) and must not overlap them in any other
  * way; dlogits_stride 0 stands for x->row_stride.  Only [rows, vocab] is written. */
 zb_status zb_token_logprobs_backward(const zb_logits* x, const float* lse, const float* dlogp, void* dlogits,

@@ -185,6 +185,7 @@ bool valid_shapes(const zb_config* c, std::string* why) {
     if (c->vocab < 1 || c->vocab > kEmbeddingMaxVocab) return bad("vocab must be in [1, 2^18]");
     if (c->loss != ZB_LOSS_CROSS_ENTROPY) {
       if (c->role != ZB_ROLE_LAST) return bad("only a last stage has a loss");
+      if ((long long)c->seq * c->mb_size > kLossMaxRows) return bad("these losses take fewer than 2^22 tokens per microbatch");
       if (c->loss == ZB_LOSS_POLICY) {
         zb_policy p{};
         p.clip_low = c->clip_low; p.clip_high = c->clip_high; p.kl_coef = c->kl_coef; p.scale = 1.0;

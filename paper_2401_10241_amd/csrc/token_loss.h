@@ -6,6 +6,7 @@
 
 namespace zb {
 
+constexpr int kLossMaxRows = (1 << 22) - 1;  // rows and pairs: a launch has less than 2^32 lanes, a row's or pair's workgroup up to 1024
 size_t loss_workspace_bytes(int rows, int pairs);
 zb_status policy_loss(const zb_logits* x, const zb_policy* p, double grad_scale, float* loss, float* logp, void* dlogits, int64_t dlogits_stride,
                       void* workspace, size_t workspace_size, hipStream_t s);

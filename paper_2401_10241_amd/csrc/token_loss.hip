@@ -630,9 +630,8 @@ __global__ __launch_bounds__(kPairThreads) void pair_kernel(PairArgs a, Rows of,
   add_up<kPairThreads>(total, part, &last);
 }
 
-constexpr int kMaxRows = (1 << 22) - 1;  // a launch has less than 2^32 lanes, a row's or pair's workgroup up to 1024
 bool valid_logits(const zb_logits* x) {
-  if (!x || x->rows < 0 || x->rows > kMaxRows || x->vocab < 1 || x->vocab > kEmbeddingMaxVocab || x->row_stride < x->vocab) return false;
+  if (!x || x->rows < 0 || x->rows > kLossMaxRows || x->vocab < 1 || x->vocab > kEmbeddingMaxVocab || x->row_stride < x->vocab) return false;
   if (x->row_stride > (int64_t)1 << 32 || (x->dtype != ZB_FP32 && x->dtype != ZB_BF16)) return false;
   if (x->rows == 0) return true;
   const uintptr_t es = x->dtype == ZB_BF16 ? 2 : 4;
@@ -753,7 +752,7 @@ bool valid_policy(const zb_policy* p) {
   return p->clip_low >= 0 && p->clip_low <= 1 && p->clip_high >= 0 && p->kl_coef >= 0 && isfinite(p->clip_high) && isfinite(p->kl_coef) && isfinite(p->scale);
 }
 bool valid_preference(const zb_preference* p) {
-  return p->pairs >= 0 && p->pairs <= kMaxRows && isfinite(p->beta) && isfinite(p->scale) && p->label_smoothing >= 0 && p->label_smoothing <= 1;
+  return p->pairs >= 0 && p->pairs <= kLossMaxRows && isfinite(p->beta) && isfinite(p->scale) && p->label_smoothing >= 0 && p->label_smoothing <= 1;
 }
 
 zb_status policy_loss(const zb_logits* x, const zb_policy* p, double grad_scale, float* loss, float* logp, void* dlogits, int64_t dlogits_stride,
@@ -834,7 +833,7 @@ zb_status zb_token_logprobs_backward(const zb_logits* x, const float* lse, const
 }
 
 zb_status zb_loss_workspace_bytes(int32_t rows, int32_t pairs, size_t* bytes) {
-  if (!bytes || rows < 0 || rows > kMaxRows || pairs < 0 || pairs > kMaxRows) return ZB_EINVAL;
+  if (!bytes || rows < 0 || rows > kLossMaxRows || pairs < 0 || pairs > kLossMaxRows) return ZB_EINVAL;
   *bytes = loss_workspace_bytes(rows, pairs);
   return ZB_OK;
 }

@@ -1,5 +1,7 @@
 """Refusals and defaults at the borders of what the operators on the caller's own device memory take; host only, no address is followed."""
 
+import ctypes as C
+
 import numpy as np
 import pytest
 
@@ -17,3 +19,21 @@ def test_numbers_that_leave_the_range_of_the_kernels(bits, bad):
     k = dict(bad)
     lr = k.pop("lr", 1e-3)
     assert rc_of(zb.adamw_step, zb.adamw_config(bits=bits, **k), zb.adamw_tensors([tensor()]), lr, AT, AT, AT) == zb.EINVAL
+
+
+@pytest.mark.parametrize("loss", [1, 2])
+def test_a_stage_of_more_tokens_than_its_loss_takes(loss):
+    """Refused when the stage is set up, not by its first F."""
+    def rc(loss, seq, mb_size):
+        cfg = zb.binding.zb_config()
+        zb.lib.zb_config_defaults(C.byref(cfg))
+        for name, value in dict(layers=1, hidden=64, heads=2, ffn=64, seq=seq, mb_size=mb_size, max_microbatches=1, max_pending_b=1, max_pending_w=1,
+                                max_inflight=1, role=2, vocab=2, loss=loss).items():
+            setattr(cfg, name, value)
+        need = C.c_size_t(0)
+        return zb.lib.zb_stage_arena_bytes(C.byref(cfg), C.byref(need))
+
+    assert rc(0, 1 << 21, 2) == rc(0, 1 << 12, 1 << 12) == zb.OK
+    for seq, mb_size in ((1 << 21, 2), (1 << 12, 1 << 10), (1 << 12, 1 << 12)):
+        assert rc(loss, seq, mb_size) == zb.EINVAL
+    assert rc(loss, (1 << 21) - 1, 2) == rc(loss, 1 << 11, (1 << 11) - 2) == zb.OK
