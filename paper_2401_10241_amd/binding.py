@@ -411,10 +411,12 @@ def adamw_config(bits: int = 32, beta1: float = 0.9, beta2: float = 0.95, eps: f
 
 
 def adamw_tensors(tensors) -> "C.Array":
-    """Array of zb_adamw_tensor from dicts of its fields (grad_dtype "fp32" or "bf16", decay on by default)."""
+    """Array of zb_adamw_tensor from dicts of its fields (grad_dtype "fp32" or "bf16", decay on by default; without `first` a
+    tensor's places follow those of the tensor before it, from 0 on: lists made apart need places of their own)."""
     out = (zb_adamw_tensor * len(tensors))()
+    place = 0
     for q, t in zip(out, tensors):
-        t = dict(t)
+        t = {"first": place, **t}
         q.grad_dtype = DTYPE[t.pop("grad_dtype", "fp32")]
         q.decay = int(t.pop("decay", True))
         for name in ("theta", "grad", "m", "v", "m_scale", "v_scale", "copy16", "n", "first"):
@@ -422,6 +424,7 @@ def adamw_tensors(tensors) -> "C.Array":
                 setattr(q, name, t.pop(name))
         if t:
             raise TypeError(f"unknown field {sorted(t)[0]!r} of an adamw tensor")
+        place = q.first + q.n
     return out
 
 

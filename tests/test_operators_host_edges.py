@@ -37,3 +37,12 @@ def test_a_stage_of_more_tokens_than_its_loss_takes(loss):
     for seq, mb_size in ((1 << 21, 2), (1 << 12, 1 << 10), (1 << 12, 1 << 12)):
         assert rc(loss, seq, mb_size) == zb.EINVAL
     assert rc(loss, (1 << 21) - 1, 2) == rc(loss, 1 << 11, (1 << 11) - 2) == zb.OK
+
+
+def test_places_of_tensors_listed_without_one():
+    """Each starts where the one before it ends, so that no two share their random numbers; a given place stays as it is."""
+    sizes = [1000, 0, 7, 300]
+    assert [t.first for t in zb.adamw_tensors([tensor(n=n) for n in sizes])] == [0, 1000, 1000, 1007]
+    assert [t.first for t in zb.adamw_tensors([tensor(n=5), tensor(n=5, first=1 << 33), tensor(n=2), tensor(n=2, first=0)])] == [0, 1 << 33, (1 << 33) + 5, 0]
+    again = [t.first for t in zb.adamw_tensors([tensor(n=3), tensor(n=4)])]
+    assert again == [0, 3]
