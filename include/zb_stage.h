@@ -366,8 +366,12 @@ zb_status zb_token_logprobs(const zb_logits* x, float* logp, float* lse, void* h
 zb_status zb_token_logprobs_backward(const zb_logits* x, const float* lse, const float* dlogp, void* dlogits,
                                      int64_t dlogits_stride, void* hip_stream);
 
-/* Scratch that the two losses need (device, 8-byte aligned, zero before its first use).
- * Calls that may run at the same time, replays of captured ones among them, need one each. */
+/* Workspace of the two losses (device, 8-byte aligned, zero before its first use).  Its first ZB_WORKSPACE_KEPT_BYTES hold a
+ * counter that the next call goes on from: they belong to the library from the first call on, and a call on a workspace in which
+ * they were overwritten may leave its result unwritten or short of parts (zeros put things right).  The rest may be used for anything between
+ * calls.  Calls that may run at the same time, replays of captured ones among them, need one each; calls one after the other may
+ * share one, of different sizes and of zb_adamw_grad_norm too. */
+#define ZB_WORKSPACE_KEPT_BYTES 64
 zb_status zb_loss_workspace_bytes(int32_t rows, int32_t pairs, size_t* bytes);
 
 /* Clipped policy loss with a KL term: with rho = exp(logp - old_logp) and d = ref_logp - logp,
@@ -432,7 +436,8 @@ typedef struct {
 
 /* Squared norm and non-finite flag of all gradients listed (theta, m, v are not looked at), as zb_grad_norm_static gives
  * them: sq_out one double, nonfinite_out one int32, both on the device; sums in a fixed order.  The workspace is device
- * memory, 8-byte aligned, zero before its first use, of its own for calls that may run at the same time. */
+ * memory under the rules of zb_loss_workspace_bytes: zero before its first use, its first ZB_WORKSPACE_KEPT_BYTES the
+ * library's from then on, one each for calls that may run at the same time. */
 zb_status zb_adamw_workspace_bytes(const zb_adamw_tensor* tensors, int32_t count, size_t* bytes);
 zb_status zb_adamw_grad_norm(const zb_adamw_tensor* tensors, int32_t count, double* sq_out, int32_t* nonfinite_out,
                              void* workspace, size_t workspace_bytes, void* hip_stream);

@@ -344,6 +344,7 @@ def grad_norm_static(grads_ptr: int, n: int, sq_out_ptr: int, nonfinite_out_ptr:
 # ---- operators of a post-training step: all pointers are device addresses (ints, 0: none), stream_handle a hipStream_t or 0 ----
 DTYPE = {"fp32": FP32, "bf16": BF16}
 ADAMW_STATE_BYTES = 64
+WORKSPACE_KEPT_BYTES = 64  # of a workspace of the losses or the norm: the library's between calls
 
 
 def logits(logits_ptr: int, rows: int, vocab: int, targets_ptr: int, dtype: str = "bf16", row_stride: int = 0) -> zb_logits:
@@ -379,7 +380,7 @@ def token_logprobs_backward(x: zb_logits, lse_ptr: int, dlogp_ptr: int, dlogits_
 
 
 def loss_workspace_bytes(rows: int, pairs: int = 0) -> int:
-    """zb_loss_workspace_bytes."""
+    """zb_loss_workspace_bytes; the first WORKSPACE_KEPT_BYTES stay as a call left them, zero before the first."""
     n = C.c_size_t(0)
     rc = lib.zb_loss_workspace_bytes(rows, pairs, C.byref(n))
     if rc != OK:

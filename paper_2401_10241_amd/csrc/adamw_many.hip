@@ -615,7 +615,7 @@ zb_status zb_adamw_grad_norm(const zb_adamw_tensor* tensors, int32_t count, doub
   OnDeviceOf on(s);
   if (!on.ok) return ZB_EDEVICE;
   const size_t parts = norm_parts(tensors, count);
-  double* sq = (double*)((char*)workspace + 64);
+  double* sq = (double*)((char*)workspace + ZB_WORKSPACE_KEPT_BYTES);
   int* nf = (int*)(sq + parts);
   const bool alone = parts > 0 && parts <= (size_t)kNormInPlace && live_tensors(tensors, count) <= kTensors;
   const NormOut out{sq_out, nonfinite_out, alone ? (unsigned*)workspace : nullptr};

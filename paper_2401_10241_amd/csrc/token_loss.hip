@@ -652,7 +652,7 @@ struct Workspace {  // a counter; per row a partial loss, the log-probability, w
 Workspace carve(void* base, int rows, int pairs) {
   Workspace w;
   w.done = (unsigned*)base;
-  w.part = (double*)((char*)base + 64);
+  w.part = (double*)((char*)base + ZB_WORKSPACE_KEPT_BYTES);
   w.logp = w.part + (rows > pairs ? rows : pairs);
   w.top = (float*)(w.logp + rows);
   w.inv = w.top + rows;
