@@ -412,8 +412,10 @@ zb_status zb_preference_loss(const zb_logits* x, const zb_preference* p, float* 
  * consecutive values of a tensor (the last block may be shorter) share one float in m_scale and one in v_scale,
  * the block's largest |m| and v:  m = sign(c) (c / 127)^2 m_scale,  v = (c / 255)^4 v_scale.  Values are rounded up or
  * down at random so that the mean is kept, by numbers made of seed, the step and the value's place first + index
- * alone: a step gives the same bits on every run, and tensors of one program should not share places.  All-zero
- * states are the states before the first step.  A tensor may be listed once only. */
+ * alone: a step gives the same bits on every run, and tensors of one program should not share places.  Two kinds of value
+ * are not held on average: a positive v below its first code, 2.4e-10 v_scale, is always raised to it (its root is divided by), and
+ * where a scale is subnormal (below 1.2e-38) values that its rounding leaves above the top code are held as the top code.
+ * All-zero states are the states before the first step.  A tensor may be listed once only. */
 typedef struct {
   float* theta;       /* parameters, fp32 */
   const void* grad;   /* their gradients */
@@ -452,8 +454,9 @@ zb_status zb_adamw_grad_norm(const zb_adamw_tensor* tensors, int32_t count, doub
 zb_status zb_adamw_step(const zb_adamw_config* cfg, const zb_adamw_tensor* tensors, int32_t count, double lr, void* state,
                         const double* sq, const int32_t* nonfinite, void* hip_stream);
 
-/* Moments held in 8 bits as fp32 values and back (each to the nearer code), e.g. for a checkpoint: values[k].m and .v
- * are device arrays of tensors[k].n floats; theta and grad are not looked at. */
+/* Moments held in 8 bits as fp32 values and back (each to the nearer code, a positive v to code 1 at least), e.g. for a
+ * checkpoint: values[k].m and .v are device arrays of tensors[k].n floats; theta and grad are not looked at.  Codes cannot hold
+ * everything: on the way back a NaN and a negative v become 0, an infinity the largest float. */
 typedef struct {
   float *m, *v;
 } zb_adamw_value;
