@@ -399,7 +399,8 @@ __global__ __launch_bounds__(THREADS, WAVES) void policy_row_kernel(const T* log
 
 // lse and log-probability, one workgroup per row: maximum and sum in one pass, U vectors of a lane at a time, the sum scaled anew when the lane's
 // maximum grows.  Bound by HBM: 4096 rows of 50432 bf16 65 us = 6.4 TB/s (with the row in registers 82).  With POLICY, for
-// rows that registers do not hold, the policy loss: the row is read again for the gradient (1536 rows of 131072 bf16 185 us).
+// rows that registers do not hold, the policy loss: the row is read again for the gradient, so its first read keeps its place in the caches whatever
+// NT (1536 rows of 131072 bf16 177 us, with the first read past the caches 214).
 template <typename T, int THREADS, int U, bool POLICY, bool NT>
 __device__ __forceinline__ void row_in_passes(const T* logits, long stride, Rows of, RowOut out, PolicyArgs pol, T* dlogits, long dstride, bool* last) {
   constexpr int VE = Span<T>::VE, N = THREADS / 64;
@@ -428,7 +429,7 @@ __device__ __forceinline__ void row_in_passes(const T* logits, long stride, Rows
   for (int k0 = lane; k0 < sp.full; k0 += U * THREADS) {
     uint4 r[U];
 #pragma unroll
-    for (int i = 0; i < U; ++i) r[i] = k0 + i * THREADS < sp.full ? get16<NT>(v + k0 + i * THREADS) : empty_pack<T>();
+    for (int i = 0; i < U; ++i) r[i] = k0 + i * THREADS < sp.full ? get16<NT && !POLICY>(v + k0 + i * THREADS) : empty_pack<T>();
     if (own_vector >= k0 && own_vector < k0 + U * THREADS) {
 #pragma unroll
       for (int i = 0; i < U; ++i)
