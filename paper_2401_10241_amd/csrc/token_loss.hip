@@ -702,9 +702,15 @@ hipError_t launch_logp(const zb_logits* x, const Rows& of, const RowOut& out, bo
 template <typename T>
 hipError_t launch_policy(const zb_logits* x, const Rows& of, const RowOut& out, const PolicyArgs& pol, void* dlogits, int64_t dstride, hipStream_t s) {
   const int vectors = x->vocab / Span<T>::VE;  // at most: a row's start may leave one fewer
-  // The fewest lanes that hold a row and leave room for a second one on the CU; WAVES per SIMD keep the registers to that.  us of 4096 rows of 32000
-  // bf16: 256 lanes 117, 512 100, 1024 105; of 50432: 256 200, 512 176, 1024 162 (with the caches' part); 2048 rows of 32000 fp32: 512 lanes
-  // 99, 1024 103, in passes 110; of 50432 fp32: 512 lanes 158 (up to 19 registers in memory), in passes 181.
+  // Shapes that hold a row in registers and leave room for a second one on the CU, WAVES per SIMD keep the registers to that.  Up to 512 x 8 vectors the
+  // fewest lanes do best; from there on twice the lanes as long as 64 registers each hold a row (1024 x 7), and then 512 again with up to 128.
+  // us of 4096 rows (fewer from 7168 vectors on), bf16 / fp32, the shape taken first:
+  //   4000 vectors   512 x 8  101 / 100   1024 x 7 109 / 98       7168 vectors  1024 x 7  154 / 153   512 x 16 169 / 154
+  //   4096           512 x 8   99 / 99    1024 x 7 111 / 100      7176          512 x 16  173 / 159   1024 x 8 164 / 155
+  //   4104          1024 x 7  115 / 102   512 x 16 134 / 114      8192          512 x 16  162 / 148   1024 x 8 166 / 151
+  //   6304          1024 x 7  155 / 154   512 x 16 177 / 162      8200          512 x 25  186 / 172   1024 x 13 227 / 185
+  // 512 x 25 keeps up to 18 registers in memory; us of it and of the row in passes: 8200 vectors 185 / 172 and 183 / 174, 10000 186 / 174 and
+  // 193 / 182, 12608 185 / 170 and 188 / 180.
 #define ZB_ROWS(THREADS, NV, WAVES)                                                                                                              \
   if (vectors <= THREADS * NV) {                                                                                                                 \
     ZB_NT((policy_row_kernel<T, THREADS, NV, WAVES, NT><<<x->rows, THREADS, 0, s>>>((const T*)x->logits, x->row_stride, of, out, pol, (T*)dlogits, \
