@@ -6,6 +6,7 @@
 #include <stdio.h>
 #include <string.h>
 
+#include <memory>
 #include <new>
 #include <string>
 #include <vector>
@@ -940,12 +941,17 @@ zb_status zb_stage_init(const zb_config* cfg, zb_stage** out) {
   st->stream = (hipStream_t)cfg->hip_stream;
   st->hp = OptHyper{cfg->lr, cfg->beta1, cfg->beta2, cfg->adam_eps, cfg->weight_decay, cfg->clip};
   for (int i = 0; i < KC_COUNT; ++i) st->prof_flops[i] = st->prof_bytes[i] = 0;
+  const size_t bounds = st->offsets ? (size_t)cfg->mb_size + 1 : 0;
+  std::unique_ptr<int[]> offsets(bounds ? new (std::nothrow) int[bounds] : nullptr);
+  if (bounds && !offsets) {
+    delete st;
+    return ZB_ENOMEM;
+  }
   // zero state: parameters, moments, gradients, journal, optimizer scalars
   hipError_t e = hipMemsetAsync(cfg->arena, 0, need, st->stream);
-  std::vector<int> offsets;
-  if (e == hipSuccess && st->offsets) {
-    for (int q = 0; q <= cfg->mb_size; ++q) offsets.push_back(q * cfg->seq);
-    e = hipMemcpyAsync(st->offsets, offsets.data(), offsets.size() * sizeof(int), hipMemcpyHostToDevice, st->stream);
+  if (e == hipSuccess && bounds) {
+    for (size_t q = 0; q < bounds; ++q) offsets[q] = (int)q * cfg->seq;
+    e = hipMemcpyAsync(st->offsets, offsets.get(), bounds * sizeof(int), hipMemcpyHostToDevice, st->stream);
   }
   if (e == hipSuccess) e = hipStreamSynchronize(st->stream);
   if (e != hipSuccess) {
