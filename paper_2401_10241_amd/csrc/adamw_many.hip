@@ -356,10 +356,10 @@ template <bool BITS8, bool WHOLE, bool NT> struct Four {
 };
 
 // One workgroup per 1024 values; which tensor they belong to stands in the launch's arguments.  32 bits: bound by HBM, 315M values with bf16
-// gradients and copies 1460 us = 6.0 TB/s (a large copy moves 4.9, a kernel that changes an array in place 5.9).  8 bits: the same 990 to 1055 us,
-// 5.1 to 4.8 TB/s, about 105 instructions a value, half of them for the codes, which the memory's 800 us do not hide all of.
-// (Two chunks a workgroup, the second's loads on their way before the first is worked on: 1057 us where one took 1044; eight values of a lane
-// instead of four: 96 registers and 1530 us.)
+// gradients and copies 1490 us = 5.9 TB/s (a large copy moves 4.9, a kernel that changes an array in place 5.9).  8 bits: the same 1024 to 1076 us,
+// 4.9 to 4.7 TB/s, about 105 instructions a value, half of them for the codes, which the memory's 800 us do not hide all of.
+// (Against 1044 us of that time: two chunks a workgroup, the second's loads on their way before the first is worked on, 1057; eight values of a lane
+// instead of four, 96 registers, 1530.)
 template <bool BITS8, bool NT>
 __global__ __launch_bounds__(kThreads) void adamw_many_kernel(Table tab, Hyper hp, const Clock* __restrict__ clk_at) {
   const Clock clk = *clk_at;
@@ -377,7 +377,7 @@ __global__ __launch_bounds__(kThreads) void adamw_many_kernel(Table tab, Hyper h
   }
 }
 
-// Moments held in 8 bits as values (bound by HBM: 315M values 500 us = 6.3 TB/s): Tensor.theta is where m's go, Tensor.grad v's
+// Moments held in 8 bits as values (bound by HBM: 315M values 502 to 527 us, 6.3 to 6.0 TB/s): Tensor.theta is where m's go, Tensor.grad v's
 __global__ __launch_bounds__(kThreads) void read_moments_kernel(Table tab) {
   const Tensor& q = tensor_of(tab, blockIdx.x);
   const long i = (long)((int)blockIdx.x - q.wg0) * kChunk + threadIdx.x * kPerThread;
@@ -396,7 +396,8 @@ __global__ __launch_bounds__(kThreads) void read_moments_kernel(Table tab) {
   store4<false>((float*)q.grad + i, live, wide, v);
 }
 
-// values into 8 bits, each to the nearer code
+// Values into 8 bits, each to the nearer code: 315M values 840 us = 3.7 TB/s, bound by the instructions of the codes set right for every value, which
+// a state that is read back once in a while does not need to be spared.
 __global__ __launch_bounds__(kThreads) void write_moments_kernel(Table tab) {
   const Tensor& q = tensor_of(tab, blockIdx.x);
   const long i = (long)((int)blockIdx.x - q.wg0) * kChunk + threadIdx.x * kPerThread;
@@ -460,9 +461,10 @@ __global__ __launch_bounds__(1024) void norm_sum_kernel(const double* __restrict
                                                         double* __restrict__ sq_out, int* __restrict__ nf_out) {
   add_parts<1024>(parts, [&](long i, double* x, int* f) { *x = part_sq[i]; *f = part_nf[i]; }, sq_out, nf_out);
 }
-// One part per workgroup; bound by HBM: 315M bf16 gradients 96 us = 6.6 TB/s (chunks of 4 / 8 / 16 / 32 times 1024 values: 123 / 105 / 102 /
-// 100).  A launch of up to kNormInPlace of them adds the parts itself: the workgroup that is through last does, reading past
-// the caches of the XCDs what the others wrote past them; `done` counts modulo the workgroups, so it is 0 again for the next call.
+// One part per workgroup; bound by HBM: 315M bf16 gradients 96 us = 6.6 TB/s.  us of the call with chunks of 4 / 8 / 16 / 32 times 1024
+// values: 109 / 101 / 99 / 97; 16 leaves twice the workgroups of 32 to shorter lists.  A launch of up to kNormInPlace of them adds the parts
+// itself: the workgroup that is through last does, reading past the caches of the XCDs what the others wrote past them; `done` counts
+// modulo the workgroups, so it is 0 again for the next call.
 template <bool NT> __global__ __launch_bounds__(kThreads) void norm_many_kernel(Table tab, double* part_sq, int* part_nf, NormOut out) {
   __shared__ double red[kThreads / 64];
   __shared__ int redf[kThreads / 64];
@@ -665,7 +667,7 @@ zb_status zb_adamw_step(const zb_adamw_config* cfg, const zb_adamw_tensor* tenso
   if (hipGetLastError() != hipSuccess) return ZB_EDEVICE;
   const bool b8 = cfg->bits == 8;
   // States that no cache would hold until the next step: more than the 256 MB of the last one.  us of 315M values with bf16 gradients with /
-  // without the caches' being told: 32 bits 1461 / 1639, 8 bits 1114 / 1132.
+  // without the caches' being told: 32 bits 1490 / 1636, 8 bits 1076 / 1110.
   double held = 0.0;
   for (int32_t k = 0; k < count; ++k) held += (double)tensors[k].n * (b8 ? 6 : 12);
   const bool nt = held > 256.0 * (1 << 20);

@@ -507,10 +507,10 @@ __global__ __launch_bounds__(THREADS) void row_kernel(const T* logits, long stri
   if (POLICY) add_up<THREADS>(out.total, out.part, &last);
 }
 
-// coef ([j = target] - exp(z_j - top) inv), inv null: 1, with the target's 1 - p from `misses` where there are any, by workgroups of kThreads * kGradVectors vectors of a row.  Bound by HBM: the rows of
-// six pairs of about 500 tokens x 50432 bf16, which have just been read for their log-probabilities, 144 us = 6.8 TB/s with the
-// rows without weight, which are not read.  us of log-probabilities and gradient with 2 / 4 / 8 vectors a lane: 229 / 239 / 258; from the
-// last row to the first, towards what the caches may still hold: 239.
+// coef ([j = target] - exp(z_j - top) inv), inv null: 1, with the target's 1 - p from `misses` where there are any, by workgroups of
+// kThreads * kGradVectors vectors of a row.  Bound by HBM: the rows of six pairs of about 500 tokens x 50432 bf16, which have just been read for
+// their log-probabilities, 144 us = 6.8 TB/s with the rows without weight, which are not read.  us of log-probabilities and gradient with 2 /
+// 4 / 8 vectors a lane: 228 / 232 / 256; from the last row to the first, towards what the caches may still hold: 232.
 constexpr int kGradVectors = 2;
 template <typename T, bool NT>
 __global__ __launch_bounds__(kThreads) void grad_kernel(const T* logits, long stride, Rows of, const float* __restrict__ coefs,
@@ -589,7 +589,7 @@ __device__ __forceinline__ void sequence_rows(const int* offsets, int q, int row
 }
 
 // One workgroup per pair: both sequences' sums of w (logp - ref), the pair's loss, and the coefficient of every row.  A chain of loads, sums
-// and one lane's exponential: 5.7 us for two pairs of 50 tokens, 8.7 for six of 500.
+// and one lane's exponential: 5.9 us for two pairs of 50 tokens, 9.0 for six of 500.
 constexpr int kPairThreads = 1024;
 __global__ __launch_bounds__(kPairThreads) void pair_kernel(PairArgs a, Rows of, int rows, const double* __restrict__ logp, float* __restrict__ rewards,
                                                             float* __restrict__ coef, double* part, Total total) {
@@ -663,8 +663,9 @@ Workspace carve(void* base, int rows, int pairs) {
 }
 
 // Lines that no cache would hold until they are wanted again: logits of over 64 MB, a quarter of the last cache (the gradient and
-// what comes next want their place in it too); where the logits are read again next, of over all of it.  us with / without:
-// log-probabilities of 4096 x 50432 bf16 69 / 74, policy loss of the same 149 / 161; 64 x 50432, read from the caches, 9.3 / 7.4 and 12.1 / 9.7.
+// what comes next want their place in it too); where the logits are read again next, of over all of it.  us with / without: log-probabilities of
+// 4096 x 50432 bf16 65 / 74, policy loss of the same 142 / 150; 768 rows (77 MB) 16.6 / 16.6 and 37 / 45, 512 rows (52 MB) 11.9 / 12.1 and 24 / 26, 64
+// rows 7.4 / 7.3 and 12.6 / 12.7: small logits lose nothing by staying.
 bool past_caches(const zb_logits* x, bool again = false) {
   return (size_t)x->rows * x->vocab * (x->dtype == ZB_BF16 ? 2 : 4) > (size_t)(again ? 256 : 64) << 20;
 }
@@ -684,9 +685,10 @@ template <typename T> hipError_t launch_logp(const zb_logits* x, const Rows& of,
     if (nt) ZB_LOGP(THREADS, U, true);                         \
     else ZB_LOGP(THREADS, U, false);                           \
   } while (0)
-  // Lanes of a workgroup by the length of a row, us of 8192 rows of 2048 / 8192 bf16 and 4096 of 32000 / 50432: 64 lanes 8.8 / - / - / -, 256
-  // 12.0 / 22.0 / 44.8 / 72.6, 512 - / 36.0 / 42.3 / 69.0, 1024 - / - / 47.2 / 73.4; 64 rows of 50432, where most of the chip is idle: 512 lanes 7.4,
-  // 1024 6.4.
+  // Lanes of a workgroup by the length of a row.  us of 8192 rows of 2048 / 4096 / 8192 / 16384 bf16 and 4096 of 32000 / 50432: 64 lanes 9.1 /
+  // 14.1, 256 lanes 19.4 / 19.1 / 22.1 / 46.9 / 50.7 / 68.5, 512 - / - / 35.1 / 49.1 / 47.4 / 65.1, 1024 55.2 / 73.9 of the last two.  Where fewer rows
+  // leave CUs idle, 512 / 1024 lanes: 100 rows of 32000 bf16 6.0 / 6.1, 50432 fp32 9.1 / 8.3, 262144 fp32 30.5 / 25.8, 511 rows of the same 9.8 / 10.1,
+  // 18.0 / 18.2, 91.5 / 93.2.
   if (vectors <= 512) ZB_ROWS(64, 4);
   else if (vectors <= 2048) ZB_ROWS(256, 4);
   else if (x->rows >= 512) ZB_ROWS(512, 4);
