@@ -270,6 +270,9 @@ template <int THREADS> __device__ __forceinline__ void add_up(const Total& t, co
   if (threadIdx.x == 0) *t.loss = (float)s;
 }
 
+// 1 - p of a target with the exponential `hit` beside `others`, inv = 1 / (hit + others); either form where it rounds less
+__device__ __forceinline__ float missed(float hit, float others, float inv) { return hit < others ? 1.f - hit * inv : others * inv; }
+
 struct RowOut {  // what the row kernels leave of a row; null: not wanted
   float *logp, *lse;
   float *top, *inv;  // p_j = exp(z_j - top) * inv
@@ -278,12 +281,12 @@ struct RowOut {  // what the row kernels leave of a row; null: not wanted
   double* part;      // with a policy: its loss
   Total total;
 };
-__device__ __forceinline__ void put_row(const RowOut& o, int row, double logp, double lse, float top, float s, float others) {
+__device__ __forceinline__ void put_row(const RowOut& o, int row, double logp, double lse, float top, float s, float hit, float others) {
   if (o.logp) o.logp[row] = (float)logp;
   if (o.lse) o.lse[row] = (float)lse;
   if (o.top) {
     const float inv = 1.0f / s;
-    o.top[row] = top; o.inv[row] = inv; o.miss[row] = others * inv;
+    o.top[row] = top; o.inv[row] = inv; o.miss[row] = missed(hit, others, inv);
   }
   if (o.logp64) o.logp64[row] = logp;
 }
@@ -357,7 +360,7 @@ __device__ __forceinline__ void policy_in_registers(const T* logits, long stride
     const double l = log_of(s64), lp = ((double)zy - (double)m) - l;
     double slope;
     loss = policy_row(pol, in, lp, &slope);
-    put_row(out, row, lp, (double)m + l, m, s, others);
+    put_row(out, row, lp, (double)m + l, m, s, exp_of(zy, m), others);
     coef_of = (float)slope;
   }
   if (dlogits) __syncthreads();
@@ -387,7 +390,7 @@ __device__ __forceinline__ void policy_in_registers(const T* logits, long stride
     }
   }
   if (edge >= 0) d[edge] = from_f32<T>(neg * exp_in<T>(xe, m));
-  if (owner) d[target] = from_f32<T>(coef * (others * inv));  // (the lane that wrote the vector around it)
+  if (owner) d[target] = from_f32<T>(coef * missed(exp_of(zy, m), others, inv));  // (the lane that wrote the vector around it)
 }
 template <typename T, int THREADS, int NV, int WAVES, bool NT>
 __global__ __launch_bounds__(THREADS, WAVES) void policy_row_kernel(const T* logits, long stride, Rows of, RowOut out, PolicyArgs pol, T* dlogits,
@@ -472,7 +475,7 @@ __device__ __forceinline__ void row_in_passes(const T* logits, long stride, Rows
       loss = policy_row(pol, terms_of(pol, of, row), lp, &slope);
       coef_of = (float)slope;
     }
-    put_row(out, row, lp, (double)m + l, m, s, others);
+    put_row(out, row, lp, (double)m + l, m, s, exp_of(zy, m), others);
   }
   if (!POLICY) return;
   if (dlogits) __syncthreads();
@@ -498,7 +501,7 @@ __device__ __forceinline__ void row_in_passes(const T* logits, long stride, Rows
     }
   }
   if (edge >= 0) d[edge] = from_f32<T>(neg * exp_in<T>(xe, m));
-  if (owner) d[target] = from_f32<T>(coef * (others * inv));  // (the lane that wrote the vector around it)
+  if (owner) d[target] = from_f32<T>(coef * missed(exp_of(zy, m), others, inv));  // (the lane that wrote the vector around it)
 }
 template <typename T, int THREADS, int U, bool POLICY, bool NT>
 __global__ __launch_bounds__(THREADS) void row_kernel(const T* logits, long stride, Rows of, RowOut out, PolicyArgs pol, T* dlogits, long dstride) {

@@ -76,3 +76,32 @@ def test_sure_tokens(dtype, shape):
     c = np.where(np.arange(rows) < rows // 2, slope, -slope)
     g = at_targets(k.gradient(), k)
     assert (np.abs(g - c * miss) <= tol(c, 0.5 * (r * np.abs(want)).sum()) + 1e-38).all(), np.abs(g - c * miss) / (np.abs(c) * miss)
+
+
+def test_targets_among_equals():
+    """All logits alike: exponentials, sums and 1 / V's numerator are exact, so a target's entry c (1 - 1 / V) carries three roundings and p's own, u / V:
+    of 1 - p, of c and of their product."""
+    import torch
+    import paper_2401_10241_amd as zb
+    rng = np.random.default_rng(21)
+    rows, worst = 96, 0.0
+    for vocab in (3, 5, 7, 11, 41, 100, 333, 1003, 5001, 40009):
+        k = Case("fp32", rows, vocab)
+        k.z[:] = 0.75
+        k.place()
+        want = -np.log(vocab)
+        old, adv = np.full(rows, want, np.float32), rng.uniform(0.1, 1.9, rows).astype(np.float32)
+        loss, ws = torch.zeros(1, device="cuda"), scratch(rows, rows // 2)
+        keep = [dev(a) for a in (old, adv, np.arange(rows + 1, dtype=np.int32), (want - adv).astype(np.float32))]
+        o, a, off, ref = (t.data_ptr() for t in keep)
+        space = dict(workspace=ws.data_ptr(), workspace_bytes=ws.numel())
+        zb.policy_loss(k.x(), zb.policy(o, a), loss.data_ptr(), 0, k.dflat.data_ptr(), **space)
+        c = -adv.astype(np.float64) * np.exp(want - old.astype(np.float64))
+        cases = [(at_targets(k.gradient(), k), c)]
+        zb.preference_loss(k.x(), zb.preference(ref, off, rows // 2, beta=0.7), loss.data_ptr(), 0, 0, k.dflat.data_ptr(), **space)
+        gap = want - (want - adv).astype(np.float32).astype(np.float64)
+        slope = -0.7 / (1 + np.exp(0.7 * (gap[0::2] - gap[1::2])))
+        cases.append((at_targets(k.gradient(), k), np.stack([slope, -slope], 1).reshape(-1)))
+        for got, c in cases:
+            off_by = np.abs(got / (c * (1 - 1 / vocab)) - 1)
+            assert (off_by <= U * (3 + 2 / vocab) + 1e-10).all(), (vocab, off_by.max() / U)  # 1e-10: the series behind c
